@@ -234,7 +234,7 @@ def _scan_plain(s):
     if not s["backward"]:
         return out
     # mu_t = f_t (g_t + mu_{t+1}), the gradient of h_{t-1}; lambda_t = g_t + mu_{t+1}, that of h_t
-    g = s["g"].float()
+    g = s["g"].to(torch.float32, copy=True)         # becomes lambda in place
     if valid is not None:
         g = torch.where(valid, g, 0.0)
     m = (f * g).flip(1)
