@@ -441,6 +441,85 @@ int pararnn_input_projection_backward(int dtype, const void *x, const float *Wx,
                                       void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
+ * The gated linear recurrence: the linear counterpart of the gated cells above (their
+ * gates without recurrent weights), whose coefficients come from the input alone,
+ *     h_l = f_l h_{l-1} + i_l v_l,     f = sig(u_f),
+ * G = 2: gates (f, v), i = 1 - f;  G = 3: gates (f, i, v), i = sig(u_i).  It is linear
+ * in h, so one scan over affine maps solves it; there is no iteration and no tolerance.
+ *   u, h, dL_dh, dL_du   [B][L][G][H] and [B][L][H] in the storage type
+ *   h0, h_last, dL_dlast, dL_dh0   the states in front of the first and behind the last step and
+ *                   their gradients, [B][H], always fp32, so that a sequence can be continued
+ *                   token by token without rounding its state.  Each may be NULL (zeros; not
+ *                   wanted), dL_dh too (zeros).  h_last may be the same memory as h0.
+ *   lengths         DEVICE int32[B] or NULL: sequence b has lengths[b] steps (taken as 0 below 0
+ *                   and as L above L).  The rows behind them are not read; they are zeros in h and
+ *                   dL_du, and the state passes them unchanged (length 0: h_last = h0).
+ *   checkpoints     of the forward call, for the backward one: the states in front of every
+ *                   tile of timesteps, pararnn_gated_checkpoint_bytes() bytes of device memory; NULL
+ *                   when no gradient is wanted.  The backward call takes them in place of h0
+ *                   and h: it recomputes the fp32 states between them.
+ *   workspace       pararnn_gated_workspace_bytes() bytes (0 on invalid arguments), for either
+ *                   direction, 256-byte aligned, no initialisation
+ * Gradients, with lam_l the gradient of h_l: lam_l = g_l + f_{l+1} lam_{l+1} (+ dL_dlast behind the
+ * last step), dv = lam i, du_i = lam v i (1 - i), du_f = lam h_{l-1} f (1 - f), for G = 2
+ * du_f = lam (h_{l-1} - v) f (1 - f), dL_dh0 = f_1 lam_1.
+ * Arithmetic in fp32; h and dL_du are rounded once.  Results are bit-reproducible.  Tensors need the alignment of their elements; 16 bytes and H a multiple of 16 bytes
+ * of elements take wide accesses.  H <= 1 048 576 (else UNSUPPORTED).  Any number of calls may run
+ * at once on workspaces of their own; a call captured into a graph may be replayed.
+ */
+size_t pararnn_gated_workspace_bytes(int dtype, int B, int L, int H, int G);
+size_t pararnn_gated_checkpoint_bytes(int dtype, int B, int L, int H, int G);
+int pararnn_gated_forward(int dtype, const void *u, const float *h0, const int *lengths, int B, int L, int H, int G,
+                          void *h, float *h_last, float *checkpoints, void *workspace, size_t workspace_bytes,
+                          void *hip_stream);
+int pararnn_gated_backward(int dtype, const void *u, const float *checkpoints, const int *lengths, const void *dL_dh,
+                           const float *dL_dlast, int B, int L, int H, int G, void *dL_du, float *dL_dh0,
+                           void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * The input projection with 4-bit weights, for serving: Wx[g][h][j] = code * scale with codes
+ * -8 .. 7 and one bf16 scale for every `group` (32, 64 or 128) consecutive inputs j of an output.
+ * G, H, n_heads, dh = H / n_heads and x, u, bias as for pararnn_input_projection; dh must be a
+ * multiple of 64 and of group, G <= 8, H <= 1 048 576 (else UNSUPPORTED).
+ *   packed          pararnn_q4_packed_bytes() = G * H * dh / 2 bytes, device, 16-byte aligned: the codes
+ *                   in the order in which the matrix cores take them (opaque)
+ *   scales          pararnn_q4_scale_bytes() = G * H * dh / group * 2 bytes, device, 2-byte aligned: bf16,
+ *                   [G * H / 16][dh / group][16]
+ * pararnn_q4_quantize: nearest values on each group's symmetric grid: scale = largest magnitude / 7
+ *   rounded to bf16, code = Wx / scale rounded to the nearest (ties to even), within -7 .. 7.  A group
+ *   of zeros has scale 0; one with an infinity or a NaN has scale NaN.
+ * pararnn_q4_pack: codes int8 [G][H][dh] (values outside -8 .. 7 are taken as the nearest of them) and
+ *   scales bf16 [G][H][dh / group] chosen elsewhere.
+ * pararnn_q4_dequantize: Wx fp32 [G][H][dh], code * scale (exact in fp32).
+ * pararnn_input_projection_q4: u = B x + bias (bias fp32 [G][H] or NULL) for any number of rows.
+ *   fp32 storage: x in full (three bf16 terms), products with the codes exact, sums in fp32.  bf16 storage: the same up to
+ *   pararnn_q4_exact_rows() rows B * L; beyond, the weights are rounded to bf16 (as pararnn_input_projection rounds its own)
+ *   into the workspace and its matrix products run.  workspace: pararnn_q4_workspace_bytes() bytes
+ *   (0 on invalid arguments), 256-byte aligned.
+ * pararnn_gated_layer_step: one token of a gated layer in one launch: the projection followed by one step
+ *   of the gated linear recurrence, h' = f h + i v with G = 2 or 3 as there.  x, y [B][H] in the storage
+ *   type, h, h_next fp32 [B][H] (may be the same memory; h NULL = zeros), y = h' rounded.  u stays in fp32
+ *   and is never written.  No workspace.
+ * There are no gradients.  Device pointers; x 16-byte aligned, the others as their elements.
+ */
+size_t pararnn_q4_packed_bytes(int H, int G, int n_heads);
+size_t pararnn_q4_scale_bytes(int H, int G, int n_heads, int group);
+int pararnn_q4_quantize(const float *Wx, int H, int G, int n_heads, int group, void *packed, void *scales,
+                        void *hip_stream);
+int pararnn_q4_pack(const signed char *codes, const void *code_scales, int H, int G, int n_heads, int group,
+                    void *packed, void *scales, void *hip_stream);
+int pararnn_q4_dequantize(const void *packed, const void *scales, int H, int G, int n_heads, int group, float *Wx,
+                          void *hip_stream);
+int pararnn_q4_exact_rows(int H, int G, int n_heads);
+size_t pararnn_q4_workspace_bytes(int dtype, int B, int L, int H, int G, int n_heads, int group);
+int pararnn_input_projection_q4(int dtype, const void *x, const void *packed, const void *scales, const float *bias,
+                                int B, int L, int H, int G, int n_heads, int group, void *u, void *workspace,
+                                size_t workspace_bytes, void *hip_stream);
+int pararnn_gated_layer_step(int dtype, const void *x, const void *packed, const void *scales, const float *bias,
+                             const float *h, int B, int H, int G, int n_heads, int group, void *y, float *h_next,
+                             void *hip_stream);
+
+/*
  * The composition kernel of the dense scan on its own (testing / profiling):
  * the products of Jacobians J_l = diag(d_l) W that Alg. 1b's update of A
  * performs, taken over chunks of pararnn_dense_chunk() consecutive timesteps,

@@ -26,7 +26,7 @@ try:
 except ImportError as e:
     raise ImportError(f"the native binding module beside {_LIB_PATH} is missing or unusable ({e}): build it with "
                       "`python -m paper_2510_21450_amd.build`") from e
-for _name in ("pararnn_input_projection", "pararnn_residual_norm", "pararnn_set_dense_jacobian", "pararnn_device_info", "pararnn_set_dense_products", "pararnn_solve_plan", "pararnn_affine_scan_workspace_bytes"):
+for _name in ("pararnn_input_projection", "pararnn_residual_norm", "pararnn_set_dense_jacobian", "pararnn_device_info", "pararnn_set_dense_products", "pararnn_solve_plan", "pararnn_affine_scan_workspace_bytes", "pararnn_gated_layer_step"):
     if not hasattr(_lib, _name):
         raise ImportError(f"{_LIB_PATH} is older than this binding ({_name} is missing): rebuild it with "
                           "`python -m paper_2510_21450_amd.build`")
@@ -415,6 +415,8 @@ def residual_norm(cell, params, u, h0, h, stream=None, out=None):
 
 _lib.pararnn_input_projection_workspace_bytes.restype = _sz
 _lib.pararnn_input_projection_workspace_bytes.argtypes = [_i] * 7
+_lib.pararnn_gated_workspace_bytes.restype = _sz
+_lib.pararnn_gated_workspace_bytes.argtypes = [_i] * 5
 
 
 def input_projection_workspace_bytes(dtype, B: int, L: int, H: int, G: int, n_heads: int = 1, backward: bool = False) -> int:
@@ -431,6 +433,63 @@ def input_projection_backward(x, Wx, du, n_heads: int = 1, want_dx: bool = True,
                               want_dbias: bool = True, workspace=None, stream=None):
     """pararnn_input_projection_backward.  Returns (dx, dWx, dbias); entries not wanted are None."""
     return _host.input_projection_backward(x, Wx, du, n_heads, want_dx, want_dw, want_dbias, workspace, _raw_stream(stream))
+
+
+def gated_workspace_bytes(dtype, B: int, L: int, H: int, G: int) -> int:
+    return _lib.pararnn_gated_workspace_bytes(DTYPES[dtype], B, L, H, G)
+
+
+def gated_forward(u, h0=None, lengths=None, checkpoints: bool = False, workspace=None, stream=None, out=None):
+    """pararnn_gated_forward: the gated linear recurrence h_t = f_t h_{t-1} + i_t v_t over whole sequences.
+    u [B][L][G][H] (fp32 or bf16) with G = 2 gates (f, v), i = 1 - f, or 3 (f, i, v); h0 fp32 [B][H] or None
+    (zeros); lengths int32 [B] or None.  Returns (h, h_last, checkpoints): h [B][L][H] of u's dtype, zeros behind
+    each sequence, h_last fp32 [B][H], and, if asked for, what `gated_backward` needs in place of the states.
+    `out` may hold a preallocated (h, h_last) pair; h_last may be h0 itself."""
+    h, last = out if out is not None else (None, None)
+    return _host.gated_forward(u, h0, lengths, checkpoints, workspace, _raw_stream(stream), h, last)
+
+
+def gated_backward(u, checkpoints, dL_dh=None, dL_dlast=None, lengths=None, want_dh0: bool = True, workspace=None, stream=None,
+                   out=None):
+    """pararnn_gated_backward.  dL_dh [B][L][H] of u's dtype and dL_dlast fp32 [B][H], either None (zeros).  Returns
+    (dL_du, dL_dh0 or None); `out` may be a preallocated dL_du."""
+    return _host.gated_backward(u, checkpoints, dL_dh, dL_dlast, lengths, want_dh0, workspace, _raw_stream(stream), out)
+
+
+#: Weights of an input projection in 4 bits (attributes packed, scales, G, H, n_heads, group), made by `quantize_projection` or
+#: `pack_projection`.
+ProjectionQ4 = _host.ProjectionQ4
+
+
+def quantize_projection(Wx, n_heads: int = 1, group: int = 64, stream=None) -> ProjectionQ4:
+    """pararnn_q4_quantize.  Wx fp32 [G][H][H / n_heads]: the nearest 4-bit values with a bf16 scale for each `group` (32, 64 or
+    128) consecutive inputs."""
+    return _host.quantize_projection(Wx, n_heads, group, _raw_stream(stream))
+
+
+def pack_projection(codes, scales, n_heads: int = 1, stream=None) -> ProjectionQ4:
+    """pararnn_q4_pack: codes int8 [G][H][H / n_heads] within -8 .. 7 and scales bf16 [G][H][H / n_heads / group] chosen
+    elsewhere."""
+    return _host.pack_projection(codes, scales, n_heads, _raw_stream(stream))
+
+
+def dequantize_projection(Wq: ProjectionQ4, stream=None):
+    """pararnn_q4_dequantize: the weights that Wq stands for, fp32 [G][H][H / n_heads]."""
+    return _host.dequantize_projection(Wq, _raw_stream(stream))
+
+
+def input_projection_q4(x, Wq: ProjectionQ4, bias=None, workspace=None, stream=None, out=None):
+    """pararnn_input_projection_q4: `input_projection` with 4-bit weights.  x [B][L][H], bias fp32 [G][H] or None ->
+    u [B][L][G][H] of x's dtype.  No gradient."""
+    return _host.input_projection_q4(x, Wq, bias, workspace, _raw_stream(stream), out)
+
+
+def gated_layer_step(x, Wq: ProjectionQ4, h=None, bias=None, stream=None, out=None):
+    """pararnn_gated_layer_step: one token of a gated layer in one launch, the projection and h' = f h + i v.
+    x [B][H], h fp32 [B][H] or None (zeros).  Returns (y, h'): y of x's dtype, h' fp32.  `out` may hold a preallocated
+    (y, h') pair; h' may be h itself.  No gradient."""
+    y, h_next = out if out is not None else (None, None)
+    return _host.gated_layer_step(x, Wq, h, bias, _raw_stream(stream), y, h_next)
 
 
 def affine_scan(J, r, reverse: bool = False, workspace=None, stream=None):

@@ -1,0 +1,696 @@
+// The gated linear recurrence h_t = f_t h_{t-1} + i_t v_t and its adjoint over whole sequences.
+//
+//   gates    G = 2: (f, v) with f = sig(u_f), i = 1 - f = sig(-u_f), v = u_v;  G = 3: (f, i, v) with i = sig(u_i)
+//   forward  the map of a stretch of steps is h -> A h + S; maps compose as (A2 A1, A2 S1 + S2)
+//   adjoint  mu_t = f_t (g_t + mu_{t+1}) is the gradient of h_{t-1}, lam_t = g_t + mu_{t+1} that of h_t:
+//            du_v = lam i,  du_i = lam v i (1 - i),  du_f = lam h_{t-1} f (1 - f)  (G = 2: lam (h_{t-1} - v) f (1 - f))
+//
+// A tile is CW channels x TT steps of one sequence.  It is read from memory once: a thread takes VEC channels of C
+// consecutive steps, 64 / LPR segments of a wave are joined by shuffles, the waves through LDS, the tiles along L by carry
+// records (look-back).  The forward pass leaves the fp32 state in front of every tile behind (checkpoints, 4 bytes a channel
+// for TT steps); the adjoint recomputes the states inside a tile from there, which reads 2 bytes a step and channel less than
+// the stored states would take and keeps their rounding out of the gradients.
+//
+// States, maps and adjoints are fp32; h and dL_du are rounded once when they are written.
+#include <algorithm>
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gated.h"
+#include "pararnn.h"
+#include "pararnn/common.h"
+#include "pararnn/launch.h"
+
+namespace pararnn {
+namespace {
+
+constexpr int kTT = 128;                 // steps of a tile
+constexpr int kCW = 64;                  // channels of a tile
+constexpr int kShort = 16;               // sequences up to this length: a thread walks them
+
+// ------------------------------------------------------------------ accesses
+typedef unsigned int u2v __attribute__((ext_vector_type(2)));
+typedef unsigned int u4v __attribute__((ext_vector_type(4)));
+
+// VEC storage elements as they lie in memory
+template <typename T, int VEC> struct Raw {
+    unsigned int w[(sizeof(T) * VEC + 3) / 4];
+    __device__ __forceinline__ float at(int k) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[k]);
+        else return __uint_as_float(k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
+    }
+};
+
+// The bounds of the resource are the bounds of the tile's valid rows: a load behind them gives zeros, a store nothing.
+// The row is part of the vector offset, which the bounds check covers (the scalar offset is outside it).
+template <typename T, int VEC> __device__ __forceinline__ Raw<T, VEC> load_raw_at(buf_rsrc r, unsigned int off)
+{
+    Raw<T, VEC> x;
+    constexpr int BYTES = sizeof(T) * VEC;
+    if constexpr (BYTES == 2) x.w[0] = __builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0);
+    else if constexpr (BYTES == 4) x.w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0);
+    else {
+        static_assert(BYTES == 16, "");
+        const u4v v = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+        x.w[0] = v.x; x.w[1] = v.y; x.w[2] = v.z; x.w[3] = v.w;
+    }
+    return x;
+}
+template <typename T, int VEC> __device__ __forceinline__ void store_at(buf_rsrc r, unsigned int off, const float (&in)[VEC])
+{
+    constexpr int BYTES = sizeof(T) * VEC;
+    unsigned int w[(BYTES + 3) / 4];
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) w[k] = __float_as_uint(in[k]);
+    } else if constexpr (VEC == 1) {
+        w[0] = f32_to_bf16(in[0]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < VEC / 2; ++k) w[k] = f32_to_bf16(in[2 * k]) | (unsigned int)f32_to_bf16(in[2 * k + 1]) << 16;
+    }
+    if constexpr (BYTES == 2) __builtin_amdgcn_raw_buffer_store_b16((unsigned short)w[0], r, off, 0, 0);
+    else if constexpr (BYTES == 4) __builtin_amdgcn_raw_buffer_store_b32(w[0], r, off, 0, 0);
+    else {
+        const u4v v = {w[0], w[1], w[2], w[3]};
+        __builtin_amdgcn_raw_buffer_store_b128(v, r, off, 0, 0);
+    }
+}
+__device__ __forceinline__ buf_rsrc rsrc_of(const void *base, unsigned int bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, bytes, 0x27000);
+}
+constexpr unsigned int kOutside = 0xfffffff0u;        // an offset behind every bound (tensors of a tile stay below 2^32 - 256 bytes)
+
+// ------------------------------------------------------------------ gates
+// f = sig(x) and 1 - f, the latter as e^-x f: exact where f rounds to 1.  e^-x is held below 2^126, so that its product with f is
+// 1 and not inf times 0 for very negative x (f is then 2^-126 instead of less).  NaN stays NaN.
+__device__ __forceinline__ void sigmoid2(float x, float *f, float *one_minus)
+{
+    float p = -1.4426950408889634f * x;
+    p = p > 126.0f ? 126.0f : p;
+    const float e = __builtin_amdgcn_exp2f(p);
+    *f = __builtin_amdgcn_rcpf(1.0f + e);
+    *one_minus = e * *f;
+}
+
+// ------------------------------------------------------------------ carry records
+// Three 64-bit words {value, tag} for a tile and channel: A and S of the tile's map, and the state behind it.  A word is written
+// and read whole and validates itself (tag = number of the call and state), so no fence is needed.
+typedef unsigned long long word_t;
+__device__ __forceinline__ void put(word_t *p, float v, unsigned int tag)
+{
+    __hip_atomic_store(p, (word_t)tag << 32 | __float_as_uint(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ word_t get(const word_t *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ bool has_tag(word_t w, unsigned int tag) { return (unsigned int)(w >> 32) == tag; }
+__device__ __forceinline__ float value(word_t w) { return __uint_as_float((unsigned int)w); }
+
+// The value that enters tile lt from its neighbours in direction dir, for one channel a lane, by a whole wave: the state behind
+// the nearest tile that has one, carried through the maps of those in between in the order and with the roundings those tiles
+// themselves use, so that the result has the same bits whichever tile that is.  U tiles are asked together, one trip to memory.
+// Tiles are numbered by a ticket in the order of their chain: every tile in front has been started by a workgroup that never
+// waits for this one, and the first of a chain publishes its state without waiting, so the wait ends.  A bound on the polls
+// ends it whatever happens; the result is then NaN.
+__device__ __forceinline__ float look_back(const word_t *rec, int dir, int lt, int n_lt, bool active, unsigned int tag_agg,
+                                           unsigned int tag_inc, unsigned int spin_limit)
+{
+    constexpr int U = 8;
+    for (unsigned int spins = 0; spins < spin_limit; ++spins) {
+        word_t a[U], s[U], x[U];
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+            const int j = lt + (q + 1) * dir;
+            const word_t *p = rec + (long long)(j >= 0 && j < n_lt ? j - lt : dir) * 3 * kCW;      // lt + dir exists
+            x[q] = get(p + 2 * kCW);
+            if (q < U - 1) { a[q] = get(p); s[q] = get(p + kCW); }
+        }
+        int found = -1;
+        bool reachable = true;
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+            const int j = lt + (q + 1) * dir;
+            if (found < 0 && reachable && j >= 0 && j < n_lt) {
+                if (__all(!active || has_tag(x[q], tag_inc))) found = q;
+                else reachable = q < U - 1 && __all(!active || (has_tag(a[q], tag_agg) && has_tag(s[q], tag_agg)));
+            }
+        }
+        if (found >= 0) {
+            float v = 0.0f;
+#pragma unroll
+            for (int q = U - 1; q >= 0; --q) {
+                if (q == found) v = value(x[q]);
+                else if (q < U - 1 && q < found) v = fmaf(value(a[q]), v, value(s[q]));
+            }
+            return active ? v : 0.0f;
+        }
+        __builtin_amdgcn_s_sleep(1);
+    }
+    return __uint_as_float(0x7fc00000u);
+}
+
+struct GatedArgs {
+    const void *u;
+    const float *h0;              // forward, or NULL
+    const int *lengths;           // or NULL
+    void *h;                      // forward: out
+    float *last;                  // forward: state behind the last step, or NULL
+    float *ckpt;                  // forward: out or NULL; backward: in
+    const void *g;                // backward, or NULL
+    const float *dlast;           // backward, or NULL
+    void *du;                     // backward: out
+    float *dh0;                   // backward: out or NULL
+    unsigned int *ticket;
+    word_t *rec;                  // [chain][tile][3][kCW]
+    unsigned int tag;             // of this call: aggregates carry tag + 1, states tag + 2
+    unsigned int spin_limit;
+    int B, L, H, n_lt, groups, chains;
+};
+
+// Where a workgroup's tile lies.
+struct Place {
+    int b, grp, lt, chain;
+    int rows, rows_all;           // valid steps, and all steps, of the tile
+};
+
+template <bool LOOK, bool REVERSE> __device__ __forceinline__ Place place_of(const GatedArgs &a, int *s_id)
+{
+    int id = (int)blockIdx.x;
+    if constexpr (LOOK) {
+        if (threadIdx.x == 0) *s_id = (int)atomicAdd(a.ticket, 1u);
+        __syncthreads();
+        id = __builtin_amdgcn_readfirstlane(*s_id);
+    }
+    Place p;
+    p.lt = LOOK ? id / a.chains : 0;
+    p.chain = id - p.lt * a.chains;
+    if (REVERSE) p.lt = a.n_lt - 1 - p.lt;
+    p.b = p.chain / a.groups;
+    p.grp = p.chain - p.b * a.groups;
+    int len = a.L;
+    if (a.lengths) {
+        len = __builtin_amdgcn_readfirstlane(a.lengths[p.b]);
+        len = len < 0 ? 0 : len > a.L ? a.L : len;
+    }
+    p.rows = len - p.lt * kTT;
+    p.rows = p.rows < 0 ? 0 : p.rows > kTT ? kTT : p.rows;
+    p.rows_all = a.L - p.lt * kTT;
+    p.rows_all = p.rows_all > kTT ? kTT : p.rows_all;
+    return p;
+}
+
+// Bytes from the tile's first channel to the end of its n rows of `width` elements.
+__device__ __forceinline__ unsigned int extent(int n, unsigned int row_bytes, unsigned int first)
+{
+    return n > 0 ? (unsigned int)n * row_bytes - first : 0u;
+}
+
+template <typename T, int G, int VEC, int W, int C, bool LOOK>
+__global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a)
+{
+    constexpr int LPR = kCW / VEC, SEG = 64 / LPR;
+    static_assert(W * SEG * C == kTT, "");
+    __shared__ float s_a[W][kCW], s_s[W][kCW], s_in[kCW];
+    __shared__ int s_id;
+    const Place p = place_of<LOOK, false>(a, &s_id);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, sg = lane / LPR, c0 = (lane % LPR) * VEC;
+    const int t0 = (w * SEG + sg) * C;
+    const unsigned int es = sizeof(T), H = (unsigned int)a.H, first = (unsigned int)p.grp * kCW;
+    const bool active = first + c0 < H;
+
+    const size_t row = (size_t)p.b * a.L + (size_t)p.lt * kTT;
+    const buf_rsrc ru = rsrc_of(static_cast<const T *>(a.u) + row * G * H + first, extent(p.rows, G * H * es, first * es));
+    Raw<T, VEC> raw[C][G];
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+            raw[j][g] = load_raw_at<T, VEC>(ru, active ? (((unsigned int)(t0 + j) * G + g) * H + c0) * es : kOutside);
+
+    float f[C][VEC], b[C][VEC], A[VEC], S[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) { A[k] = 1.0f; S[k] = 0.0f; }
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+        const bool valid = t0 + j < p.rows;
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            float ff, om, i;
+            sigmoid2(raw[j][0].at(k), &ff, &om);
+            i = om;
+            if constexpr (G == 3) i = fast_sigmoid(raw[j][1].at(k));
+            f[j][k] = valid ? ff : 1.0f;
+            b[j][k] = valid ? i * raw[j][G - 1].at(k) : 0.0f;
+            A[k] *= f[j][k];
+            S[k] = fmaf(f[j][k], S[k], b[j][k]);
+        }
+    }
+    // maps of the wave's segments up to and including this one, then without it
+#pragma unroll
+    for (int d = LPR; d < 64; d *= 2)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            const float a1 = __shfl_up(A[k], d, 64), s1 = __shfl_up(S[k], d, 64);
+            if (lane >= d) {
+                S[k] = fmaf(A[k], s1, S[k]);
+                A[k] *= a1;
+            }
+        }
+    if (sg == SEG - 1)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) { s_a[w][c0 + k] = A[k]; s_s[w][c0 + k] = S[k]; }
+    if constexpr (SEG > 1) {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            const float a1 = __shfl_up(A[k], LPR, 64), s1 = __shfl_up(S[k], LPR, 64);
+            A[k] = sg ? a1 : 1.0f;
+            S[k] = sg ? s1 : 0.0f;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) { A[k] = 1.0f; S[k] = 0.0f; }
+    }
+    __syncthreads();
+    if (w == 0) {                                            // a lane for each channel of the tile
+        const unsigned int ch = first + lane;
+        const bool act = ch < H;
+        float ta = 1.0f, ts = 0.0f;
+#pragma unroll
+        for (int q = 0; q < W; ++q) { ts = fmaf(s_a[q][lane], ts, s_s[q][lane]); ta *= s_a[q][lane]; }
+        float in = 0.0f;
+        word_t *rec = a.rec + ((size_t)p.chain * a.n_lt + p.lt) * (3 * kCW) + lane;
+        if (!LOOK || p.lt == 0) {
+            if (a.h0 && act) in = a.h0[(size_t)p.b * H + ch];
+        } else {
+            if (act && p.lt + 1 < a.n_lt) { put(rec, ta, a.tag + 1); put(rec + kCW, ts, a.tag + 1); }
+            in = look_back(rec, -1, p.lt, a.n_lt, act, a.tag + 1, a.tag + 2, a.spin_limit);
+        }
+        const float out = fmaf(ta, in, ts);
+        if (LOOK && act && p.lt + 1 < a.n_lt) put(rec + 2 * kCW, out, a.tag + 2);
+        s_in[lane] = in;
+        if (a.ckpt && act) a.ckpt[((size_t)p.b * a.n_lt + p.lt) * H + ch] = in;
+        if (a.last && act && p.lt + 1 == a.n_lt) a.last[(size_t)p.b * H + ch] = out;
+    }
+    // this wave's place among the waves, while the first one waits
+    float x[VEC], pa[VEC], ps[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) { pa[k] = 1.0f; ps[k] = 0.0f; }
+    for (int q = 0; q < w; ++q)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) { ps[k] = fmaf(s_a[q][c0 + k], ps[k], s_s[q][c0 + k]); pa[k] *= s_a[q][c0 + k]; }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) x[k] = fmaf(A[k], fmaf(pa[k], s_in[c0 + k], ps[k]), S[k]);
+
+    const buf_rsrc rh = rsrc_of(static_cast<T *>(a.h) + row * H + first, extent(p.rows_all, H * es, first * es));
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+        const bool valid = t0 + j < p.rows;
+        float o[VEC];
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            x[k] = fmaf(f[j][k], x[k], b[j][k]);
+            o[k] = valid ? x[k] : 0.0f;
+        }
+        store_at<T, VEC>(rh, active ? ((unsigned int)(t0 + j) * H + c0) * es : kOutside, o);
+    }
+}
+
+template <typename T, int G, int VEC, int W, int C, bool LOOK>
+__global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedArgs a)
+{
+    constexpr int LPR = kCW / VEC, SEG = 64 / LPR;
+    static_assert(W * SEG * C == kTT, "");
+    __shared__ float s_a[W][kCW], s_s[W][kCW], s_m[W][kCW], s_in[kCW];
+    __shared__ int s_id;
+    const Place p = place_of<LOOK, true>(a, &s_id);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, sg = lane / LPR, c0 = (lane % LPR) * VEC;
+    const int t0 = (w * SEG + sg) * C;
+    const unsigned int es = sizeof(T), H = (unsigned int)a.H, first = (unsigned int)p.grp * kCW;
+    const bool active = first + c0 < H;
+
+    const size_t row = (size_t)p.b * a.L + (size_t)p.lt * kTT;
+    const buf_rsrc ru = rsrc_of(static_cast<const T *>(a.u) + row * G * H + first, extent(p.rows, G * H * es, first * es));
+    const buf_rsrc rg = rsrc_of(static_cast<const T *>(a.g) + row * H + first, extent(a.g ? p.rows : 0, H * es, first * es));
+    Raw<T, VEC> raw[C][G], rawg[C];
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+            raw[j][g] = load_raw_at<T, VEC>(ru, active ? (((unsigned int)(t0 + j) * G + g) * H + c0) * es : kOutside);
+        rawg[j] = load_raw_at<T, VEC>(rg, active ? ((unsigned int)(t0 + j) * H + c0) * es : kOutside);
+    }
+    float before[VEC];                                       // the state in front of the tile
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) before[k] = active ? a.ckpt[((size_t)p.b * a.n_lt + p.lt) * H + first + c0 + k] : 0.0f;
+
+    float f[C][VEC], om[C][VEC], i[C][VEC], A[VEC], S[VEC], M[VEC], RA[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) { A[k] = 1.0f; S[k] = M[k] = 0.0f; }
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+        const bool valid = t0 + j < p.rows;
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            sigmoid2(raw[j][0].at(k), &f[j][k], &om[j][k]);
+            if (!valid) { f[j][k] = 1.0f; om[j][k] = 0.0f; }
+            i[j][k] = om[j][k];
+            if constexpr (G == 3) i[j][k] = valid ? fast_sigmoid(raw[j][1].at(k)) : 0.0f;
+            A[k] *= f[j][k];
+            S[k] = fmaf(f[j][k], S[k], i[j][k] * raw[j][G - 1].at(k));       // behind the valid steps v is loaded as zero
+        }
+    }
+#pragma unroll
+    for (int j = C - 1; j >= 0; --j)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) M[k] = f[j][k] * (rawg[j].at(k) + M[k]);
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) RA[k] = A[k];
+    // along time for the states, against it for the adjoint
+#pragma unroll
+    for (int d = LPR; d < 64; d *= 2)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            const float a1 = __shfl_up(A[k], d, 64), s1 = __shfl_up(S[k], d, 64);
+            const float a2 = __shfl_down(RA[k], d, 64), m2 = __shfl_down(M[k], d, 64);
+            if (lane >= d) {
+                S[k] = fmaf(A[k], s1, S[k]);
+                A[k] *= a1;
+            }
+            if (lane + d < 64) {
+                M[k] = fmaf(RA[k], m2, M[k]);
+                RA[k] *= a2;
+            }
+        }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+        if (sg == SEG - 1) { s_a[w][c0 + k] = A[k]; s_s[w][c0 + k] = S[k]; }
+        if (sg == 0) s_m[w][c0 + k] = M[k];
+    }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+        if constexpr (SEG > 1) {
+            const float a1 = __shfl_up(A[k], LPR, 64), s1 = __shfl_up(S[k], LPR, 64);
+            const float a2 = __shfl_down(RA[k], LPR, 64), m2 = __shfl_down(M[k], LPR, 64);
+            A[k] = sg ? a1 : 1.0f;
+            S[k] = sg ? s1 : 0.0f;
+            RA[k] = sg + 1 < SEG ? a2 : 1.0f;
+            M[k] = sg + 1 < SEG ? m2 : 0.0f;
+        } else {
+            A[k] = RA[k] = 1.0f;
+            S[k] = M[k] = 0.0f;
+        }
+    }
+    __syncthreads();
+    if (w == 0) {
+        const unsigned int ch = first + lane;
+        const bool act = ch < H;
+        float ta = 1.0f, tm = 0.0f;
+#pragma unroll
+        for (int q = W - 1; q >= 0; --q) { tm = fmaf(s_a[q][lane], tm, s_m[q][lane]); ta *= s_a[q][lane]; }
+        float in = 0.0f;
+        word_t *rec = a.rec + ((size_t)p.chain * a.n_lt + p.lt) * (3 * kCW) + lane;
+        if (!LOOK || p.lt + 1 == a.n_lt) {
+            if (a.dlast && act) in = a.dlast[(size_t)p.b * H + ch];
+        } else {
+            if (act && p.lt > 0) { put(rec, ta, a.tag + 1); put(rec + kCW, tm, a.tag + 1); }
+            in = look_back(rec, 1, p.lt, a.n_lt, act, a.tag + 1, a.tag + 2, a.spin_limit);
+        }
+        const float out = fmaf(ta, in, tm);
+        if (LOOK && act && p.lt > 0) put(rec + 2 * kCW, out, a.tag + 2);
+        s_in[lane] = in;
+        if (a.dh0 && act && p.lt == 0) a.dh0[(size_t)p.b * H + ch] = out;
+    }
+    // the state in front of this thread's steps, and in front of each of them
+    float hp[C][VEC];
+    for (int q = 0; q < w; ++q)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) before[k] = fmaf(s_a[q][c0 + k], before[k], s_s[q][c0 + k]);
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) before[k] = fmaf(A[k], before[k], S[k]);
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            hp[j][k] = before[k];
+            before[k] = fmaf(f[j][k], before[k], i[j][k] * raw[j][G - 1].at(k));
+        }
+    float pa[VEC], pm[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) { pa[k] = 1.0f; pm[k] = 0.0f; }
+    for (int q = W - 1; q > w; --q)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) { pm[k] = fmaf(s_a[q][c0 + k], pm[k], s_m[q][c0 + k]); pa[k] *= s_a[q][c0 + k]; }
+    __syncthreads();
+    float m[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) m[k] = fmaf(RA[k], fmaf(pa[k], s_in[c0 + k], pm[k]), M[k]);
+
+    const buf_rsrc rd = rsrc_of(static_cast<T *>(a.du) + row * G * H + first, extent(p.rows_all, G * H * es, first * es));
+#pragma unroll
+    for (int j = C - 1; j >= 0; --j) {
+        const bool valid = t0 + j < p.rows;
+        float o[G][VEC];
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            const float lam = rawg[j].at(k) + m[k], v = raw[j][G - 1].at(k);
+            const float slope = f[j][k] * om[j][k];
+            o[G - 1][k] = valid ? lam * i[j][k] : 0.0f;
+            if constexpr (G == 2) {
+                o[0][k] = valid ? lam * (hp[j][k] - v) * slope : 0.0f;
+            } else {
+                // 1 - i from the gate's input: exact where i rounds to 1
+                o[0][k] = valid ? lam * hp[j][k] * slope : 0.0f;
+                o[1][k] = valid ? lam * v * i[j][k] * fast_sigmoid(-raw[j][1].at(k)) : 0.0f;
+            }
+            m[k] = f[j][k] * lam;
+        }
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+            store_at<T, VEC>(rd, active ? (((unsigned int)(t0 + j) * G + g) * H + c0) * es : kOutside, o[g]);
+    }
+}
+
+// A few steps: a thread walks them for VEC channels.  One launch, no workspace; bound by latency.
+template <typename T, int G, int VEC> __global__ __launch_bounds__(256) void gated_walk_kernel(const GatedArgs a)
+{
+    const int per_row = a.H / VEC;
+    const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (id >= (long long)a.B * per_row) return;
+    const int b = (int)(id / per_row), c0 = (int)(id - (long long)b * per_row) * VEC;
+    int len = a.L;
+    if (a.lengths) {
+        len = a.lengths[b];
+        len = len < 0 ? 0 : len > a.L ? a.L : len;
+    }
+    const T *u = static_cast<const T *>(a.u) + (size_t)b * a.L * G * a.H + c0;
+    T *h = static_cast<T *>(a.h) + (size_t)b * a.L * a.H + c0;
+    auto read = [](const T *p) {
+        Raw<T, VEC> x;
+        if constexpr (sizeof(x) == 16) *reinterpret_cast<u4v *>(x.w) = *reinterpret_cast<const u4v *>(p);
+        else if constexpr (sizeof(T) == 4) x.w[0] = *reinterpret_cast<const unsigned int *>(p);
+        else x.w[0] = *reinterpret_cast<const unsigned short *>(p);
+        return x;
+    };
+    float x[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+        x[k] = a.h0 ? a.h0[(size_t)b * a.H + c0 + k] : 0.0f;
+        if (a.ckpt) a.ckpt[(size_t)b * a.H + c0 + k] = x[k];
+    }
+    for (int t = 0; t < a.L; ++t) {
+        float o[VEC];
+        if (t < len) {
+            Raw<T, VEC> r[G];
+#pragma unroll
+            for (int g = 0; g < G; ++g) r[g] = read(u + ((size_t)t * G + g) * a.H);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) {
+                float f, i;
+                sigmoid2(r[0].at(k), &f, &i);
+                if constexpr (G == 3) i = fast_sigmoid(r[1].at(k));
+                x[k] = fmaf(f, x[k], i * r[G - 1].at(k));
+                o[k] = x[k];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) o[k] = 0.0f;
+        }
+        T *at = h + (size_t)t * a.H;
+        if constexpr (sizeof(T) == 4) {
+            if constexpr (VEC == 4) *reinterpret_cast<float4 *>(at) = make_float4(o[0], o[1], o[2], o[3]);
+            else *at = o[0];
+        } else if constexpr (VEC == 8) {
+            unsigned int w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = f32_to_bf16(o[2 * k]) | (unsigned int)f32_to_bf16(o[2 * k + 1]) << 16;
+            *reinterpret_cast<uint4 *>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+            *at = f32_to_bf16(o[0]);
+        }
+    }
+    if (a.last)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) a.last[(size_t)b * a.H + c0 + k] = x[k];
+}
+
+__global__ __launch_bounds__(256) void gated_clear_kernel(ulonglong2 *p, size_t n)
+{
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = make_ulonglong2(0, 0);
+}
+
+// ------------------------------------------------------------------ host
+struct Shape {
+    int n_lt, groups;
+    long long chains, tiles;
+    size_t bytes;                 // control block, and carry records where there is more than one tile along L
+};
+
+bool shape_of(int dtype, int B, int L, int H, int G, Shape *s)
+{
+    if ((dtype != PARARNN_F32 && dtype != PARARNN_BF16) || B < 1 || L < 1 || H < 1 || (G != 2 && G != 3)) return false;
+    s->n_lt = (int)(((long long)L + kTT - 1) / kTT);
+    s->groups = (H + kCW - 1) / kCW;
+    s->chains = (long long)B * s->groups;
+    s->tiles = s->chains * s->n_lt;
+    s->bytes = 256 + (s->n_lt > 1 ? (size_t)s->tiles * 3 * kCW * sizeof(word_t) : 0);
+    return true;
+}
+
+// Row offsets of a tile are 32-bit (128 steps x 3 gates x 4 bytes x 2^20 channels), tile numbers too.
+bool size_ok(const Shape &s, int H) { return H <= (1 << 20) && s.tiles < (1ll << 31); }
+
+bool wide_ok(int H, int dtype, std::initializer_list<const void *> ptrs)
+{
+    uintptr_t m = 0;
+    for (const void *p : ptrs) m |= (uintptr_t)p;
+    return m % 16 == 0 && H % (dtype == PARARNN_BF16 ? 8 : 4) == 0;
+}
+
+hipError_t launch_clear(void *ws, size_t bytes, hipStream_t st)
+{
+    const size_t n = bytes / 16;
+    const size_t blocks = std::min<size_t>((n + 255) / 256, (size_t)std::max(1, device_cu_count()) * 8);
+    hipLaunchKernelGGL(gated_clear_kernel, dim3((unsigned)blocks), dim3(256), 0, st, static_cast<ulonglong2 *>(ws), n);
+    return hipGetLastError();
+}
+
+template <typename T, int G> hipError_t launch_forward(const GatedArgs &a, bool wide, unsigned blocks, hipStream_t st)
+{
+    constexpr int V = 16 / sizeof(T);
+    const bool look = a.n_lt > 1;
+    if (wide) {
+        constexpr int C = kTT / (4 * (64 * V / kCW));
+        if (look) hipLaunchKernelGGL((gated_forward_kernel<T, G, V, 4, C, true>), dim3(blocks), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((gated_forward_kernel<T, G, V, 4, C, false>), dim3(blocks), dim3(256), 0, st, a);
+    } else {
+        if (look) hipLaunchKernelGGL((gated_forward_kernel<T, G, 1, 8, kTT / 8, true>), dim3(blocks), dim3(512), 0, st, a);
+        else hipLaunchKernelGGL((gated_forward_kernel<T, G, 1, 8, kTT / 8, false>), dim3(blocks), dim3(512), 0, st, a);
+    }
+    return hipGetLastError();
+}
+
+template <typename T, int G> hipError_t launch_backward(const GatedArgs &a, bool wide, unsigned blocks, hipStream_t st)
+{
+    constexpr int V = 16 / sizeof(T);
+    const bool look = a.n_lt > 1;
+    if (wide) {
+        constexpr int C = kTT / (8 * (64 * V / kCW));
+        if (look) hipLaunchKernelGGL((gated_backward_kernel<T, G, V, 8, C, true>), dim3(blocks), dim3(512), 0, st, a);
+        else hipLaunchKernelGGL((gated_backward_kernel<T, G, V, 8, C, false>), dim3(blocks), dim3(512), 0, st, a);
+    } else {
+        if (look) hipLaunchKernelGGL((gated_backward_kernel<T, G, 1, 8, kTT / 8, true>), dim3(blocks), dim3(512), 0, st, a);
+        else hipLaunchKernelGGL((gated_backward_kernel<T, G, 1, 8, kTT / 8, false>), dim3(blocks), dim3(512), 0, st, a);
+    }
+    return hipGetLastError();
+}
+
+template <typename T, int G> hipError_t launch_walk(const GatedArgs &a, bool wide, hipStream_t st)
+{
+    constexpr int V = 16 / sizeof(T);
+    const long long n = (long long)a.B * (a.H / (wide ? V : 1));
+    const unsigned blocks = (unsigned)((n + 255) / 256);
+    if (wide) hipLaunchKernelGGL((gated_walk_kernel<T, G, V>), dim3(blocks), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((gated_walk_kernel<T, G, 1>), dim3(blocks), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+bool misaligned(const void *p, size_t n) { return (uintptr_t)p % n != 0; }
+
+}  // namespace
+
+size_t gated_workspace_bytes(int dtype, int B, int L, int H, int G)
+{
+    Shape s;
+    return shape_of(dtype, B, L, H, G, &s) && size_ok(s, H) ? s.bytes : 0;
+}
+
+size_t gated_checkpoint_bytes(int dtype, int B, int L, int H, int G)
+{
+    Shape s;
+    return shape_of(dtype, B, L, H, G, &s) && size_ok(s, H) ? (size_t)B * s.n_lt * H * sizeof(float) : 0;
+}
+
+int gated_forward(int dtype, const void *u, const float *h0, const int *lengths, int B, int L, int H, int G, void *h,
+                  float *h_last, float *checkpoints, void *workspace, size_t workspace_bytes, hipStream_t st)
+{
+    Shape s;
+    if (!shape_of(dtype, B, L, H, G, &s) || !u || !h || !workspace || misaligned(workspace, 256)) return PARARNN_INVALID_ARG;
+    const size_t es = dtype == PARARNN_BF16 ? 2 : 4;
+    if (misaligned(u, es) || misaligned(h, es) || misaligned(h0, 4) || misaligned(lengths, 4) || misaligned(h_last, 4) ||
+        misaligned(checkpoints, 4))
+        return PARARNN_INVALID_ARG;
+    if (!size_ok(s, H)) return PARARNN_UNSUPPORTED;
+    if (workspace_bytes < s.bytes) return PARARNN_WORKSPACE_TOO_SMALL;
+    GatedArgs a = {};
+    a.u = u; a.h0 = h0; a.lengths = lengths; a.h = h; a.last = h_last; a.ckpt = checkpoints;
+    a.B = B; a.L = L; a.H = H; a.n_lt = s.n_lt; a.groups = s.groups; a.chains = (int)s.chains;
+    const bool wide = wide_ok(H, dtype, {u, h});
+    if (L <= kShort) {
+        const hipError_t e = dtype == PARARNN_BF16 ? (G == 2 ? launch_walk<unsigned short, 2>(a, wide, st) : launch_walk<unsigned short, 3>(a, wide, st))
+                                                   : (G == 2 ? launch_walk<float, 2>(a, wide, st) : launch_walk<float, 3>(a, wide, st));
+        return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
+    }
+    char *ws = static_cast<char *>(workspace);
+    a.ticket = reinterpret_cast<unsigned int *>(ws);
+    a.rec = reinterpret_cast<word_t *>(ws + 256);
+    a.tag = 0; a.spin_limit = kSpinLimit;
+    if (s.n_lt > 1 && launch_clear(ws, s.bytes, st) != hipSuccess) return PARARNN_HIP_ERROR;
+    const unsigned blocks = (unsigned)s.tiles;
+    const hipError_t e = dtype == PARARNN_BF16
+                             ? (G == 2 ? launch_forward<unsigned short, 2>(a, wide, blocks, st) : launch_forward<unsigned short, 3>(a, wide, blocks, st))
+                             : (G == 2 ? launch_forward<float, 2>(a, wide, blocks, st) : launch_forward<float, 3>(a, wide, blocks, st));
+    return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
+}
+
+int gated_backward(int dtype, const void *u, const float *checkpoints, const int *lengths, const void *dL_dh,
+                   const float *dL_dlast, int B, int L, int H, int G, void *dL_du, float *dL_dh0, void *workspace,
+                   size_t workspace_bytes, hipStream_t st)
+{
+    Shape s;
+    if (!shape_of(dtype, B, L, H, G, &s) || !u || !checkpoints || !dL_du || !workspace || misaligned(workspace, 256))
+        return PARARNN_INVALID_ARG;
+    const size_t es = dtype == PARARNN_BF16 ? 2 : 4;
+    if (misaligned(u, es) || misaligned(dL_dh, es) || misaligned(dL_du, es) || misaligned(checkpoints, 4) || misaligned(lengths, 4) ||
+        misaligned(dL_dlast, 4) || misaligned(dL_dh0, 4))
+        return PARARNN_INVALID_ARG;
+    if (!size_ok(s, H)) return PARARNN_UNSUPPORTED;
+    if (workspace_bytes < s.bytes) return PARARNN_WORKSPACE_TOO_SMALL;
+    GatedArgs a = {};
+    a.u = u; a.lengths = lengths; a.ckpt = const_cast<float *>(checkpoints); a.g = dL_dh; a.dlast = dL_dlast; a.du = dL_du; a.dh0 = dL_dh0;
+    a.B = B; a.L = L; a.H = H; a.n_lt = s.n_lt; a.groups = s.groups; a.chains = (int)s.chains;
+    const bool wide = wide_ok(H, dtype, {u, dL_dh, dL_du});
+    char *ws = static_cast<char *>(workspace);
+    a.ticket = reinterpret_cast<unsigned int *>(ws);
+    a.rec = reinterpret_cast<word_t *>(ws + 256);
+    a.tag = 0; a.spin_limit = kSpinLimit;
+    if (s.n_lt > 1 && launch_clear(ws, s.bytes, st) != hipSuccess) return PARARNN_HIP_ERROR;
+    const unsigned blocks = (unsigned)s.tiles;
+    const hipError_t e = dtype == PARARNN_BF16
+                             ? (G == 2 ? launch_backward<unsigned short, 2>(a, wide, blocks, st) : launch_backward<unsigned short, 3>(a, wide, blocks, st))
+                             : (G == 2 ? launch_backward<float, 2>(a, wide, blocks, st) : launch_backward<float, 3>(a, wide, blocks, st));
+    return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
+}
+
+}  // namespace pararnn

@@ -3,6 +3,8 @@
 // device about 10 us; checks, allocations and ctypes marshalling in Python took 15 us of host time on top of the call.
 // No arithmetic here, and no device code: everything runs in the kernels behind pararnn.h.
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
+#include <c10/core/StreamGuard.h>
 #include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/custom_function.h>
@@ -426,6 +428,230 @@ ProjGrads project_backward(const Tensor &x, const Tensor &Wx, const Tensor &du, 
     return r;
 }
 
+// ------------------------------------------------------------------ gated linear recurrence, 4-bit weights
+// These calls run on the device of their tensors, whichever is current, and on the caller's stream if there is one: what they
+// allocate belongs to the stream that uses it.
+class On {
+public:
+    On(const Tensor &t, const char *name, const c10::optional<int64_t> &stream)
+    {
+        if (!t.is_cuda()) throw py::value_error(std::string(name) + " must be a CUDA tensor");
+        guard_.reset_device(t.device());
+        auto s = stream ? c10::hip::getStreamFromExternal(reinterpret_cast<hipStream_t>(*stream), t.get_device())
+                        : c10::hip::getCurrentHIPStream(t.get_device());
+        if (stream) on_.emplace(s.unwrap());
+        stream_ = static_cast<void *>(s.stream());
+    }
+    void *stream() const { return stream_; }
+
+private:
+    c10::OptionalDeviceGuard guard_;
+    c10::optional<c10::StreamGuard> on_;
+    void *stream_;
+};
+
+void check_on(const Tensor &t, const char *name, at::ScalarType dtype, at::IntArrayRef shape, const Tensor &like)
+{
+    check(t, name, dtype, shape);
+    if (t.device() != like.device()) throw py::value_error(std::string(name) + " must be on " + like.device().str() + ", got " + t.device().str());
+}
+
+int int_of(int64_t n, const char *name)
+{
+    if (n < 0 || n > 0x7fffffff) throw py::value_error(std::string(name) + " is out of range");
+    return (int)n;
+}
+
+struct GatedDims { int B, L, G, H; };
+GatedDims gated_dims(const Tensor &u)
+{
+    if (u.dim() != 4) throw py::value_error("u must have four dimensions");
+    const GatedDims d = {int_of(u.size(0), "u"), int_of(u.size(1), "u"), int_of(u.size(2), "u"), int_of(u.size(3), "u")};
+    check(u, "u", u.scalar_type());
+    if (d.G != 2 && d.G != 3) throw py::value_error("u must have 2 or 3 gates, got " + std::to_string(d.G));
+    return d;
+}
+
+struct GatedOut { Tensor h, last, ckpt; };
+
+GatedOut gated_solve(const Tensor &u, const OptTensor &h0, const OptTensor &lengths, bool checkpoints, const OptTensor &workspace,
+                     const c10::optional<int64_t> &stream, const OptTensor &out, const OptTensor &out_last)
+{
+    const On on(u, "u", stream);
+    const GatedDims d = gated_dims(u);
+    const auto dt = u.scalar_type();
+    const int code = dtype_code(dt);
+    if (has(h0)) check_on(*h0, "h0", at::kFloat, {d.B, d.H}, u);
+    if (has(lengths)) check_on(*lengths, "lengths", at::kInt, {d.B}, u);
+    GatedOut r;
+    r.h = has(out) ? *out : at::empty({d.B, d.L, d.H}, u.options());
+    check_on(r.h, "h", dt, {d.B, d.L, d.H}, u);
+    r.last = has(out_last) ? *out_last : at::empty({d.B, d.H}, u.options().dtype(at::kFloat));
+    check_on(r.last, "h_last", at::kFloat, {d.B, d.H}, u);
+    if (checkpoints) {
+        const size_t bytes = pararnn_gated_checkpoint_bytes(code, d.B, d.L, d.H, d.G);
+        const int64_t rows = bytes ? (int64_t)(bytes / 4 / d.B / d.H) : 0;
+        r.ckpt = at::empty({d.B, rows, d.H}, u.options().dtype(at::kFloat));
+    }
+    const Tensor ws = workspace_of(pararnn_gated_workspace_bytes(code, d.B, d.L, d.H, d.G), u, workspace);
+    raise_if(pararnn_gated_forward(code, u.data_ptr(), static_cast<const float *>(ptr(h0)), static_cast<const int *>(ptr(lengths)), d.B,
+                                   d.L, d.H, d.G, r.h.data_ptr(), static_cast<float *>(r.last.data_ptr()),
+                                   checkpoints ? static_cast<float *>(r.ckpt.data_ptr()) : nullptr, ws.data_ptr(), (size_t)ws.numel(),
+                                   on.stream()),
+             "pararnn_gated_forward");
+    return r;
+}
+
+struct GatedGrads { Tensor du, dh0; };
+
+GatedGrads gated_adjoint(const Tensor &u, const Tensor &ckpt, const OptTensor &g, const OptTensor &dlast, const OptTensor &lengths,
+                         bool want_dh0, const OptTensor &workspace, const c10::optional<int64_t> &stream, const OptTensor &out)
+{
+    const On on(u, "u", stream);
+    const GatedDims d = gated_dims(u);
+    const auto dt = u.scalar_type();
+    const int code = dtype_code(dt);
+    const size_t bytes = pararnn_gated_checkpoint_bytes(code, d.B, d.L, d.H, d.G);
+    check_on(ckpt, "checkpoints", at::kFloat, {d.B, bytes ? (int64_t)(bytes / 4 / d.B / d.H) : 0, d.H}, u);
+    if (has(g)) check_on(*g, "dL_dh", dt, {d.B, d.L, d.H}, u);
+    if (has(dlast)) check_on(*dlast, "dL_dlast", at::kFloat, {d.B, d.H}, u);
+    if (has(lengths)) check_on(*lengths, "lengths", at::kInt, {d.B}, u);
+    GatedGrads r;
+    r.du = has(out) ? *out : at::empty(u.sizes(), u.options());
+    check_on(r.du, "dL_du", dt, u.sizes(), u);
+    if (want_dh0) r.dh0 = at::empty({d.B, d.H}, u.options().dtype(at::kFloat));
+    const Tensor ws = workspace_of(pararnn_gated_workspace_bytes(code, d.B, d.L, d.H, d.G), u, workspace);
+    raise_if(pararnn_gated_backward(code, u.data_ptr(), static_cast<const float *>(ckpt.data_ptr()), static_cast<const int *>(ptr(lengths)),
+                                    ptr(g), static_cast<const float *>(ptr(dlast)), d.B, d.L, d.H, d.G, r.du.data_ptr(),
+                                    want_dh0 ? static_cast<float *>(r.dh0.data_ptr()) : nullptr, ws.data_ptr(), (size_t)ws.numel(),
+                                    on.stream()),
+             "pararnn_gated_backward");
+    return r;
+}
+
+// 4-bit weights as the Python side holds them
+struct Q4 {
+    Tensor packed, scales;
+    int G, H, heads, group;
+};
+
+struct Q4Shape { int G, H, dh, heads; };
+Q4Shape q4_shape(const Tensor &W, const char *name, at::ScalarType dtype, int64_t n_heads)
+{
+    if (W.dim() != 3) throw py::value_error(std::string(name) + " must have three dimensions");
+    if (n_heads < 1) throw py::value_error("n_heads must be positive");
+    const Q4Shape s = {int_of(W.size(0), name), int_of(W.size(1), name), int_of(W.size(1) / n_heads, name), int_of(n_heads, "n_heads")};
+    check(W, name, dtype, {s.G, s.H, s.dh});
+    if ((int64_t)s.dh * n_heads != s.H) throw py::value_error("n_heads must divide H");
+    return s;
+}
+
+Q4 q4_empty(const Q4Shape &s, int64_t group, const Tensor &like)
+{
+    Q4 q;
+    q.G = s.G; q.H = s.H; q.heads = s.heads; q.group = int_of(group, "group");
+    q.packed = at::empty({(int64_t)pararnn_q4_packed_bytes(s.H, s.G, s.heads)}, like.options().dtype(at::kByte));
+    q.scales = at::empty({(int64_t)pararnn_q4_scale_bytes(s.H, s.G, s.heads, q.group) / 2}, like.options().dtype(at::kBFloat16));
+    return q;
+}
+
+// Refuses what the library would before anything is allocated: an empty buffer has no address.
+void q4_supported(const Q4Shape &s, int64_t group)
+{
+    if (group != 32 && group != 64 && group != 128) throw py::value_error("group must be 32, 64 or 128, got " + std::to_string(group));
+    if (s.G < 1 || s.G > 8) throw py::value_error("there must be 1 to 8 gates, got " + std::to_string(s.G));
+    if (pararnn_q4_scale_bytes(s.H, s.G, s.heads, (int)group) == 0)
+        throw py::value_error("channels per head must be a multiple of 64 and of group, H at most 1048576");
+}
+
+Q4 q4_quantize(const Tensor &W, int64_t n_heads, int64_t group, const c10::optional<int64_t> &stream)
+{
+    const On on(W, "Wx", stream);
+    const Q4Shape s = q4_shape(W, "Wx", at::kFloat, n_heads);
+    q4_supported(s, group);
+    Q4 q = q4_empty(s, group, W);
+    raise_if(pararnn_q4_quantize(static_cast<const float *>(W.data_ptr()), s.H, s.G, s.heads, q.group, q.packed.data_ptr(),
+                                 q.scales.data_ptr(), on.stream()),
+             "pararnn_q4_quantize");
+    return q;
+}
+
+Q4 q4_pack(const Tensor &codes, const Tensor &scales, int64_t n_heads, const c10::optional<int64_t> &stream)
+{
+    const On on(codes, "codes", stream);
+    const Q4Shape s = q4_shape(codes, "codes", at::kChar, n_heads);
+    const int64_t n = scales.dim() == 3 ? scales.size(2) : 0, group = n > 0 && s.dh % n == 0 ? s.dh / n : 0;
+    q4_supported(s, group);
+    check_on(scales, "scales", at::kBFloat16, {s.G, s.H, n}, codes);
+    Q4 q = q4_empty(s, group, codes);
+    raise_if(pararnn_q4_pack(static_cast<const signed char *>(codes.data_ptr()), scales.data_ptr(), s.H, s.G, s.heads, q.group,
+                             q.packed.data_ptr(), q.scales.data_ptr(), on.stream()),
+             "pararnn_q4_pack");
+    return q;
+}
+
+void q4_check(const Q4 &q, const Tensor &like)
+{
+    check_on(q.packed, "packed", at::kByte, {(int64_t)pararnn_q4_packed_bytes(q.H, q.G, q.heads)}, like);
+    check_on(q.scales, "scales", at::kBFloat16, {(int64_t)pararnn_q4_scale_bytes(q.H, q.G, q.heads, q.group) / 2}, like);
+}
+
+Tensor q4_dequantize(const Q4 &q, const c10::optional<int64_t> &stream)
+{
+    const On on(q.packed, "packed", stream);
+    q4_check(q, q.packed);
+    Tensor W = at::empty({q.G, q.H, q.H / q.heads}, q.packed.options().dtype(at::kFloat));
+    raise_if(pararnn_q4_dequantize(q.packed.data_ptr(), q.scales.data_ptr(), q.H, q.G, q.heads, q.group,
+                                   static_cast<float *>(W.data_ptr()), on.stream()),
+             "pararnn_q4_dequantize");
+    return W;
+}
+
+Tensor q4_project(const Tensor &x, const Q4 &q, const OptTensor &bias, const OptTensor &workspace, const c10::optional<int64_t> &stream,
+                  const OptTensor &out)
+{
+    const On on(x, "x", stream);
+    if (x.dim() != 3) throw py::value_error("x must have three dimensions");
+    const auto dt = x.scalar_type();
+    const int code = dtype_code(dt), B = int_of(x.size(0), "x"), L = int_of(x.size(1), "x");
+    check(x, "x", dt, {B, L, q.H});
+    q4_check(q, x);
+    if (has(bias)) check_on(*bias, "bias", at::kFloat, {q.G, q.H}, x);
+    Tensor u = has(out) ? *out : at::empty({B, L, q.G, q.H}, x.options());
+    check_on(u, "u", dt, {B, L, q.G, q.H}, x);
+    const Tensor ws = workspace_of(pararnn_q4_workspace_bytes(code, B, L, q.H, q.G, q.heads, q.group), x, workspace);
+    raise_if(pararnn_input_projection_q4(code, x.data_ptr(), q.packed.data_ptr(), q.scales.data_ptr(), static_cast<const float *>(ptr(bias)),
+                                         B, L, q.H, q.G, q.heads, q.group, u.data_ptr(), ws.data_ptr(), (size_t)ws.numel(), on.stream()),
+             "pararnn_input_projection_q4");
+    return u;
+}
+
+struct StepOut { Tensor y, h; };
+
+StepOut gated_step(const Tensor &x, const Q4 &q, const OptTensor &h, const OptTensor &bias, const c10::optional<int64_t> &stream,
+                   const OptTensor &out, const OptTensor &out_h)
+{
+    const On on(x, "x", stream);
+    if (x.dim() != 2) throw py::value_error("x must have two dimensions");
+    const auto dt = x.scalar_type();
+    const int code = dtype_code(dt), B = int_of(x.size(0), "x");
+    check(x, "x", dt, {B, q.H});
+    q4_check(q, x);
+    if (q.G != 2 && q.G != 3) throw py::value_error("the weights must have 2 or 3 gates, got " + std::to_string(q.G));
+    if (has(h)) check_on(*h, "h", at::kFloat, {B, q.H}, x);
+    if (has(bias)) check_on(*bias, "bias", at::kFloat, {q.G, q.H}, x);
+    StepOut r;
+    r.y = has(out) ? *out : at::empty({B, q.H}, x.options());
+    check_on(r.y, "y", dt, {B, q.H}, x);
+    r.h = has(out_h) ? *out_h : at::empty({B, q.H}, x.options().dtype(at::kFloat));
+    check_on(r.h, "h_next", at::kFloat, {B, q.H}, x);
+    raise_if(pararnn_gated_layer_step(code, x.data_ptr(), q.packed.data_ptr(), q.scales.data_ptr(), static_cast<const float *>(ptr(bias)),
+                                      static_cast<const float *>(ptr(h)), B, q.H, q.G, q.heads, q.group, r.y.data_ptr(),
+                                      static_cast<float *>(r.h.data_ptr()), on.stream()),
+             "pararnn_gated_layer_step");
+    return r;
+}
+
 // ------------------------------------------------------------------ autograd
 using torch::autograd::AutogradContext;
 using torch::autograd::variable_list;
@@ -527,6 +753,92 @@ struct Layer : torch::autograd::Function<Layer> {
     }
 };
 
+// A backward pass that is captured into a graph while another graph, built on another stream, keeps the accumulators of the same
+// leaves alive: the engine would make that stream wait for the captured one, which draws it into the capture and ends the
+// process when the capture ends.  Refused before anything is launched; what this node returns is what it would wait for.
+void refuse_foreign_leaves(std::initializer_list<Tensor> inputs)
+{
+    const auto cur = c10::hip::getCurrentHIPStream();
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(cur.stream(), &cap) != hipSuccess || cap == hipStreamCaptureStatusNone) return;
+    for (const Tensor &t : inputs) {
+        if (!t.defined() || !t.requires_grad() || !t.is_leaf()) continue;
+        const auto node = torch::autograd::impl::try_get_grad_accumulator(t);
+        const auto stream = node ? node->stream() : c10::nullopt;
+        // (by number: the same stream is of another device type by name in either half of torch)
+        if (stream && (stream->id() != cur.id() || stream->device_index() != cur.device_index()))
+            throw std::runtime_error("a backward pass cannot be captured into a graph while an eager graph of the same leaves is alive: "
+                                     "release that graph (its outputs) first");
+    }
+}
+
+// The gated linear recurrence: gated_forward with gated_backward as its gradient.
+struct Gated : torch::autograd::Function<Gated> {
+    static variable_list forward(AutogradContext *ctx, Tensor u, OptTensor h0, OptTensor lengths, bool train)
+    {
+        GatedOut r = gated_solve(u, h0, lengths, train, {}, {}, {}, {});
+        if (train) ctx->save_for_backward({u, r.ckpt, or_none(lengths), or_none(h0)});
+        ctx->set_materialize_grads(false);
+        return {r.h, r.last};
+    }
+    static variable_list backward(AutogradContext *ctx, variable_list grads)
+    {
+        variable_list out(4);
+        if (!grads[0].defined() && !grads[1].defined()) return out;
+        const auto v = ctx->get_saved_variables();
+        refuse_foreign_leaves({v[0], v[3]});
+        Edges need{ctx};
+        need(true);
+        const bool nh = need(v[3].defined());
+        GatedGrads g = gated_adjoint(v[0], v[1], dense(grads[0]), dense(grads[1]), v[2], nh, {}, {}, {});
+        out[0] = g.du; out[1] = g.dh0;
+        return out;
+    }
+    static OptTensor dense(const Tensor &g) { return g.defined() ? OptTensor(g.contiguous()) : OptTensor(); }
+};
+
+// The projection followed by the gated linear recurrence, as one node.
+struct GatedLayer : torch::autograd::Function<GatedLayer> {
+    static variable_list forward(AutogradContext *ctx, Tensor x, Tensor Wx, OptTensor bias, OptTensor h0, OptTensor lengths, int64_t n_heads,
+                                 bool train)
+    {
+        const On on(x, "x", {});
+        Tensor u = project(x, Wx, bias, n_heads, {}, {}, {});
+        GatedOut r = gated_solve(u, h0, lengths, train, {}, {}, {}, {});
+        if (train) ctx->save_for_backward({x, Wx, u, r.ckpt, or_none(lengths), or_none(bias), or_none(h0)});
+        ctx->saved_data["n_heads"] = n_heads;
+        ctx->set_materialize_grads(false);
+        return {r.h, r.last};
+    }
+    static variable_list backward(AutogradContext *ctx, variable_list grads)
+    {
+        variable_list out(7);
+        if (!grads[0].defined() && !grads[1].defined()) return out;
+        const auto v = ctx->get_saved_variables();
+        const On on(v[0], "x", {});
+        refuse_foreign_leaves({v[0], v[1], v[5], v[6]});
+        Edges need{ctx};
+        const bool nx = need(true), nw = need(true), nb = need(v[5].defined()), nh = need(v[6].defined());
+        GatedGrads g = gated_adjoint(v[2], v[3], Gated::dense(grads[0]), Gated::dense(grads[1]), v[4], nh, {}, {}, {});
+        out[3] = g.dh0;
+        if (nx || nw || nb) {
+            ProjGrads p = project_backward(v[0], v[1], g.du, ctx->saved_data["n_heads"].toInt(), nx, nw || nb, nb, {}, {});
+            out[0] = p.dx;
+            if (nw) out[1] = p.dW;
+            out[2] = p.db;
+        }
+        return out;
+    }
+};
+
+bool wants_grad(std::initializer_list<const OptTensor *> ts)
+{
+    if (!at::GradMode::is_enabled()) return false;
+    for (const OptTensor *t : ts)
+        if (has(*t) && (*t)->requires_grad()) return true;
+    return false;
+}
+
 // Runs a call into the library without the interpreter lock: it may allocate, and wait for a place in a full launch queue.
 template <class F> auto unlocked(F &&f)
 {
@@ -600,5 +912,51 @@ PYBIND11_MODULE(_host, m)
                           const OptTensor &h0, int64_t n_heads, double tol, int64_t max_iter) {
         variable_list r = unlocked([&] { return Layer::apply(x, Wx, bias, params, h0, c, n_heads, tol, max_iter); });
         return py::make_tuple(r[0], r[1]);
+    });
+    m.def("gated_forward", [](const Tensor &u, const OptTensor &h0, const OptTensor &lengths, bool checkpoints, const OptTensor &workspace,
+                              const c10::optional<int64_t> &stream, const OptTensor &out, const OptTensor &out_last) {
+        GatedOut r = unlocked([&] { return gated_solve(u, h0, lengths, checkpoints, workspace, stream, out, out_last); });
+        return py::make_tuple(r.h, r.last, object_of(r.ckpt));
+    });
+    m.def("gated_backward", [](const Tensor &u, const Tensor &ckpt, const OptTensor &g, const OptTensor &dlast, const OptTensor &lengths,
+                               bool want_dh0, const OptTensor &workspace, const c10::optional<int64_t> &stream, const OptTensor &out) {
+        GatedGrads r = unlocked([&] { return gated_adjoint(u, ckpt, g, dlast, lengths, want_dh0, workspace, stream, out); });
+        return py::make_tuple(r.du, object_of(r.dh0));
+    });
+    m.def("gated_apply", [](const Tensor &u, const OptTensor &h0, const OptTensor &lengths) {
+        variable_list r = unlocked([&] {
+            const OptTensor ou(u);
+            return Gated::apply(u, h0, lengths, wants_grad({&ou, &h0}));
+        });
+        return py::make_tuple(r[0], r[1]);
+    });
+    m.def("gated_layer", [](const Tensor &x, const Tensor &Wx, const OptTensor &bias, const OptTensor &h0, const OptTensor &lengths,
+                            int64_t n_heads) {
+        variable_list r = unlocked([&] {
+            const OptTensor ox(x), ow(Wx);
+            return GatedLayer::apply(x, Wx, bias, h0, lengths, n_heads, wants_grad({&ox, &ow, &bias, &h0}));
+        });
+        return py::make_tuple(r[0], r[1]);
+    });
+    py::class_<Q4>(m, "ProjectionQ4", "Weights of an input projection in 4 bits, with a bf16 scale for each group of inputs.")
+        .def_readonly("packed", &Q4::packed).def_readonly("scales", &Q4::scales)
+        .def_readonly("G", &Q4::G).def_readonly("H", &Q4::H).def_readonly("n_heads", &Q4::heads).def_readonly("group", &Q4::group);
+    m.def("quantize_projection", [](const Tensor &W, int64_t n_heads, int64_t group, const c10::optional<int64_t> &stream) {
+        return unlocked([&] { return q4_quantize(W, n_heads, group, stream); });
+    });
+    m.def("pack_projection", [](const Tensor &codes, const Tensor &scales, int64_t n_heads, const c10::optional<int64_t> &stream) {
+        return unlocked([&] { return q4_pack(codes, scales, n_heads, stream); });
+    });
+    m.def("dequantize_projection", [](const Q4 &q, const c10::optional<int64_t> &stream) {
+        return unlocked([&] { return q4_dequantize(q, stream); });
+    });
+    m.def("input_projection_q4", [](const Tensor &x, const Q4 &q, const OptTensor &bias, const OptTensor &workspace,
+                                    const c10::optional<int64_t> &stream, const OptTensor &out) {
+        return unlocked([&] { return q4_project(x, q, bias, workspace, stream, out); });
+    });
+    m.def("gated_layer_step", [](const Tensor &x, const Q4 &q, const OptTensor &h, const OptTensor &bias, const c10::optional<int64_t> &stream,
+                                 const OptTensor &out, const OptTensor &out_h) {
+        StepOut r = unlocked([&] { return gated_step(x, q, h, bias, stream, out, out_h); });
+        return py::make_tuple(r.y, r.h);
     });
 }

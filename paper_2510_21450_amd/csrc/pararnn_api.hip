@@ -9,7 +9,9 @@
 #include "dense.h"
 #include "cells.h"
 #include "pararnn/driver.h"
+#include "gated.h"
 #include "proj.h"
+#include "q4.h"
 
 using namespace pararnn;
 
@@ -596,6 +598,69 @@ int pararnn_input_projection_backward(int dtype, const void *x, const float *Wx,
     workspace_forget(workspace);
     return proj_backward(dtype, x, Wx, du, B, L, H, G, n_heads, dx, dWx, dbias, workspace, workspace_bytes,
                          static_cast<hipStream_t>(hip_stream));
+}
+
+size_t pararnn_gated_workspace_bytes(int dtype, int B, int L, int H, int G) { return gated_workspace_bytes(dtype, B, L, H, G); }
+
+size_t pararnn_gated_checkpoint_bytes(int dtype, int B, int L, int H, int G) { return gated_checkpoint_bytes(dtype, B, L, H, G); }
+
+int pararnn_gated_forward(int dtype, const void *u, const float *h0, const int *lengths, int B, int L, int H, int G, void *h,
+                          float *h_last, float *checkpoints, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    workspace_forget(workspace);
+    return gated_forward(dtype, u, h0, lengths, B, L, H, G, h, h_last, checkpoints, workspace, workspace_bytes,
+                         static_cast<hipStream_t>(hip_stream));
+}
+
+int pararnn_gated_backward(int dtype, const void *u, const float *checkpoints, const int *lengths, const void *dL_dh,
+                           const float *dL_dlast, int B, int L, int H, int G, void *dL_du, float *dL_dh0, void *workspace,
+                           size_t workspace_bytes, void *hip_stream)
+{
+    workspace_forget(workspace);
+    return gated_backward(dtype, u, checkpoints, lengths, dL_dh, dL_dlast, B, L, H, G, dL_du, dL_dh0, workspace, workspace_bytes,
+                          static_cast<hipStream_t>(hip_stream));
+}
+
+size_t pararnn_q4_packed_bytes(int H, int G, int n_heads) { return q4_packed_bytes(H, G, n_heads); }
+
+size_t pararnn_q4_scale_bytes(int H, int G, int n_heads, int group) { return q4_scale_bytes(H, G, n_heads, group); }
+
+int pararnn_q4_quantize(const float *Wx, int H, int G, int n_heads, int group, void *packed, void *scales, void *hip_stream)
+{
+    return q4_quantize(Wx, H, G, n_heads, group, packed, scales, static_cast<hipStream_t>(hip_stream));
+}
+
+int pararnn_q4_pack(const signed char *codes, const void *code_scales, int H, int G, int n_heads, int group, void *packed,
+                    void *scales, void *hip_stream)
+{
+    return q4_pack(codes, code_scales, H, G, n_heads, group, packed, scales, static_cast<hipStream_t>(hip_stream));
+}
+
+int pararnn_q4_dequantize(const void *packed, const void *scales, int H, int G, int n_heads, int group, float *Wx, void *hip_stream)
+{
+    return q4_dequantize(packed, scales, H, G, n_heads, group, Wx, static_cast<hipStream_t>(hip_stream));
+}
+
+int pararnn_q4_exact_rows(int H, int G, int n_heads) { return q4_exact_rows(H, G, n_heads); }
+
+size_t pararnn_q4_workspace_bytes(int dtype, int B, int L, int H, int G, int n_heads, int group)
+{
+    return q4_workspace_bytes(dtype, B, L, H, G, n_heads, group);
+}
+
+int pararnn_input_projection_q4(int dtype, const void *x, const void *packed, const void *scales, const float *bias, int B, int L,
+                                int H, int G, int n_heads, int group, void *u, void *workspace, size_t workspace_bytes,
+                                void *hip_stream)
+{
+    workspace_forget(workspace);
+    return q4_project(dtype, x, packed, scales, bias, B, L, H, G, n_heads, group, u, workspace, workspace_bytes,
+                      static_cast<hipStream_t>(hip_stream));
+}
+
+int pararnn_gated_layer_step(int dtype, const void *x, const void *packed, const void *scales, const float *bias, const float *h,
+                             int B, int H, int G, int n_heads, int group, void *y, float *h_next, void *hip_stream)
+{
+    return q4_step(dtype, x, packed, scales, bias, h, B, H, G, n_heads, group, y, h_next, static_cast<hipStream_t>(hip_stream));
 }
 
 int pararnn_dense_chunk(void) { return dense_chunk(); }

@@ -2412,26 +2412,17 @@ size_t proj_workspace_bytes(int dtype, int B, int L, int H, int G, int n_heads, 
     return proj_layout(dtype, B, L, H, G, n_heads, backward).total;
 }
 
-int proj_forward(int dtype, const void *x, const float *Wx, const float *bias, int B, int L, int H, int G,
-                 int n_heads, void *u, void *workspace, size_t workspace_bytes, hipStream_t st)
+// tickets, then the weights in bf16: the same places for every problem
+unsigned short *proj_weights_at(void *workspace, int **tickets)
 {
-    if (!shapes_ok(dtype, B, L, H, G, n_heads)) return PARARNN_INVALID_ARG;
+    *tickets = static_cast<int *>(workspace);
+    return reinterpret_cast<unsigned short *>(static_cast<char *>(workspace) + 256);
+}
+
+int proj_product(int dtype, const void *x, const unsigned short *Wb, const float *bias, int B, int L, int H, int G, int n_heads,
+                 void *u, int *tickets, hipStream_t st)
+{
     const int dh = H / n_heads;
-    if (dh % BK) return PARARNN_UNSUPPORTED;
-    if (((uintptr_t)x | (uintptr_t)Wx | (uintptr_t)u | (uintptr_t)workspace) % 16) return PARARNN_UNSUPPORTED;
-    const ProjLayout lo = proj_layout(dtype, B, L, H, G, n_heads, 0);
-    if (workspace_bytes < lo.total) return PARARNN_WORKSPACE_TOO_SMALL;
-    RowsArgs r;
-    int blocks;
-    if (rows_shape(B * L, H, G, n_heads, dtype == PARARNN_BF16, &r, &blocks)) {
-        r.x = x; r.Wx = Wx; r.bias = bias; r.u = u;
-        const hipError_t e = dtype == PARARNN_BF16 ? launch_rows<unsigned short>(r, dh / 64, blocks, st) : launch_rows<float>(r, dh / 64, blocks, st);
-        return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
-    }
-    unsigned short *Wb = reinterpret_cast<unsigned short *>(static_cast<char *>(workspace) + lo.off_w);
-    const size_t nw = (size_t)G * H * dh;
-    int *tickets = reinterpret_cast<int *>(static_cast<char *>(workspace) + lo.off_tickets);
-    hipLaunchKernelGGL(proj_wb_kernel, dim3(elementwise_blocks(nw / 4)), dim3(256), 0, st, Wx, Wb, nw / 4, tickets);
     GemmArgs g;
     memset(&g, 0, sizeof(g));
     g.A = x; g.Bw = Wb; g.C = u; g.bias = bias; g.tickets = tickets;
@@ -2448,6 +2439,29 @@ int proj_forward(int dtype, const void *x, const float *Wx, const float *bias, i
                              ? ((g_proj_dma && nt_dma_f32_ok(g) && G <= 3) ? launch_nt_dma_f32(g, st) : launch_nt<float, float>(g, st))
                          : (g_proj_dma && nt_dma_ok(g)) ? launch_nt_dma(g, st) : launch_nt<unsigned short, unsigned short>(g, st);
     return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
+}
+
+int proj_forward(int dtype, const void *x, const float *Wx, const float *bias, int B, int L, int H, int G,
+                 int n_heads, void *u, void *workspace, size_t workspace_bytes, hipStream_t st)
+{
+    if (!shapes_ok(dtype, B, L, H, G, n_heads)) return PARARNN_INVALID_ARG;
+    const int dh = H / n_heads;
+    if (dh % BK) return PARARNN_UNSUPPORTED;
+    if (((uintptr_t)x | (uintptr_t)Wx | (uintptr_t)u | (uintptr_t)workspace) % 16) return PARARNN_UNSUPPORTED;
+    const ProjLayout lo = proj_layout(dtype, B, L, H, G, n_heads, 0);
+    if (workspace_bytes < lo.total) return PARARNN_WORKSPACE_TOO_SMALL;
+    RowsArgs r;
+    int blocks;
+    if (rows_shape(B * L, H, G, n_heads, dtype == PARARNN_BF16, &r, &blocks)) {
+        r.x = x; r.Wx = Wx; r.bias = bias; r.u = u;
+        const hipError_t e = dtype == PARARNN_BF16 ? launch_rows<unsigned short>(r, dh / 64, blocks, st) : launch_rows<float>(r, dh / 64, blocks, st);
+        return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
+    }
+    int *tickets = nullptr;
+    unsigned short *Wb = proj_weights_at(workspace, &tickets);
+    const size_t nw = (size_t)G * H * dh;
+    hipLaunchKernelGGL(proj_wb_kernel, dim3(elementwise_blocks(nw / 4)), dim3(256), 0, st, Wx, Wb, nw / 4, tickets);
+    return proj_product(dtype, x, Wb, bias, B, L, H, G, n_heads, u, tickets, st);
 }
 
 int proj_backward(int dtype, const void *x, const float *Wx, const void *du, int B, int L, int H, int G, int n_heads,

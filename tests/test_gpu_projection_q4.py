@@ -1,0 +1,275 @@
+"""4-bit weights of the input projection, their products and the gated layer's single step on the GPU against plain 64-bit
+forms on the CPU."""
+import pytest
+import torch
+
+import gated_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def P():
+    import paper_2510_21450_amd as P
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    return P
+
+
+def weights(G, heads, dh, seed):
+    gen = torch.Generator().manual_seed(seed)
+    return torch.randn(G, heads * dh, dh, generator=gen) * dh ** -0.5
+
+
+def bound(x, W, scales, heads, rounded_weights=False):
+    """Error of u from sums in fp32: the products with a code's 24 + q and the 24 taken out (together below 56 of scale s for
+    each |x|), at most 64 + dh / 32 roundings of a running sum on the way; bf16 weights: half a step each."""
+    G, H, dh = W.shape
+    s = scales.double().repeat_interleave(dh // scales.shape[-1], -1)
+    e = ref.project(x.double().abs(), s * 56 * (64 + dh / 32) * ref.EPS, None, heads)
+    if rounded_weights:
+        e = e + ref.project(x.double().abs(), W.abs() * 2.0 ** -8, None, heads)
+    return e
+
+
+# ---------------------------------------------------------------- quantising
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("G,heads,dh", [(1, 1, 128), (2, 3, 128), (3, 1, 256), (1, 2, 384)])
+def test_nearest_values(P, G, heads, dh, group):
+    W = weights(G, heads, dh, seed=dh + group)
+    Wq = P.quantize_projection(W.cuda(), n_heads=heads, group=group)
+    codes, scales = ref.quantise(W, group)
+    assert (Wq.G, Wq.H, Wq.n_heads, Wq.group) == (G, heads * dh, heads, group)
+    assert torch.equal(P.dequantize_projection(Wq).cpu().double(), ref.values(codes, scales))
+    packed = P.pack_projection(codes.cuda(), scales.cuda(), n_heads=heads)
+    assert torch.equal(packed.packed, Wq.packed)
+    assert torch.equal(packed.scales.view(torch.int16), Wq.scales.view(torch.int16))
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_values_at_the_borders(P, group):
+    """Ties, one step beside them, groups of zeros, of subnormals, of one value, with an infinity, with a NaN; rows at a
+    4-byte address."""
+    W = torch.zeros(1, 128, 128)
+    s = 0.0078125 * 1.25                                    # a bf16 number; 7 s is the largest of each group below
+    mid = (torch.arange(32, dtype=torch.float32) % 7 + 0.5) * s
+    W[0, 0:16] = mid.repeat(4)
+    W[0, 16:32] = torch.nextafter(mid, torch.tensor(1e9)).repeat(4)
+    W[0, 32:48] = torch.nextafter(mid, torch.tensor(-1e9)).repeat(4)
+    W[0, 0:48, ::32] = 7 * s
+    W[0, 8:48:2] *= -1
+    W[0, 48] = 1e-41
+    W[0, 49, 3] = 3.4e38
+    W[0, 50, 5] = float("inf")
+    W[0, 51, 127] = float("nan")
+    W[0, 52, 64] = -2.5
+    flat = torch.empty(W.numel() + 1, device="cuda")
+    view = flat[1:].view(W.shape)
+    view.copy_(W)
+    got = P.dequantize_projection(P.quantize_projection(view, group=group)).cpu().double()
+    codes, scales = ref.quantise(W, group)
+    want = ref.values(codes, scales)
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(got.nan_to_num(0.0), want.nan_to_num(0.0))
+
+
+def test_codes_from_elsewhere(P):
+    """All sixteen codes, and what lies outside them; negative and zero scales."""
+    gen = torch.Generator().manual_seed(2)
+    codes = torch.randint(-12, 12, (2, 128, 64), generator=gen, dtype=torch.int8)
+    scales = torch.randn(2, 128, 2, generator=gen).to(torch.bfloat16)
+    scales[0, 3, 1] = 0.0
+    got = P.dequantize_projection(P.pack_projection(codes.cuda(), scales.cuda(), n_heads=2)).cpu().double()
+    assert torch.equal(got, ref.values(codes.clamp(-8, 7), scales))
+
+
+# ---------------------------------------------------------------- products
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("G,heads,dh,group", [(1, 1, 64, 32), (3, 3, 64, 64), (2, 2, 128, 128), (4, 1, 192, 64), (2, 1, 576, 32), (1, 2, 640, 128)])
+@pytest.mark.parametrize("rows", [1, 5, 16, 17, 33, 64, 65, 130])
+def test_products(P, rows, G, heads, dh, group, dtype):
+    gen = torch.Generator().manual_seed(rows + dh)
+    W = weights(G, heads, dh, seed=rows)
+    codes, scales = ref.quantise(W, group)
+    codes[0, 0, :8] = -8
+    x = torch.randn(rows, heads * dh, generator=gen).to(dtype)
+    bias = torch.randn(G, heads * dh, generator=gen) if rows % 2 else None
+    Wq = P.pack_projection(codes.cuda(), scales.cuda(), n_heads=heads)
+    B = 5 if rows % 5 == 0 else 1
+    u = P.input_projection_q4(x.view(B, rows // B, -1).cuda(), Wq, None if bias is None else bias.cuda())
+    V = ref.values(codes, scales)
+    want = ref.project(x, V, bias, heads)
+    many = dtype == torch.bfloat16 and rows > 64
+    err = bound(x, V, scales, heads, rounded_weights=many) + 4 * ref.EPS * (0 if bias is None else bias.double().abs())
+    ref.check(u.view(rows, G, -1), want, err, "u")
+
+
+def test_one_row_of_another_batch_is_the_same(P):
+    """A sequence's pre-activations do not depend on how many others there are beside it (bits, up to the exact rows)."""
+    W = weights(3, 2, 256, seed=4).cuda()
+    Wq = P.quantize_projection(W, n_heads=2, group=64)
+    x = torch.randn(64, 1, 512, generator=torch.Generator().manual_seed(4)).cuda()
+    alone = P.input_projection_q4(x[:1].contiguous(), Wq)
+    for n in (2, 16):
+        assert torch.equal(P.input_projection_q4(x[:n].contiguous(), Wq)[:1], alone)
+
+
+def test_unaligned_outputs_and_rows_behind(P):
+    """u at an element's alignment only, with guards around it that stay as they are."""
+    Wq = P.quantize_projection(weights(2, 1, 128, seed=6).cuda(), group=32)
+    for dtype in (torch.float32, torch.bfloat16):
+        x = torch.randn(3, 1, 128, generator=torch.Generator().manual_seed(6)).to(dtype).cuda()
+        flat = torch.full((1 + 3 * 256 + 7,), 5.0, dtype=dtype, device="cuda")
+        u = P.input_projection_q4(x, Wq, out=flat[1:1 + 3 * 256].view(3, 1, 2, 128))
+        assert torch.equal(u, P.input_projection_q4(x, Wq))
+        assert (flat[:1] == 5).all() and (flat[1 + 3 * 256:] == 5).all()
+
+
+# ---------------------------------------------------------------- a token of a gated layer
+def step_reference(x, V, scales, h, bias, heads, G):
+    u = ref.project(x, V, bias, heads)
+    e = bound(x, V, scales, heads) + 4 * ref.EPS * (0 if bias is None else bias.double().abs())
+    f, i, v = ref.gates(u)
+    s = torch.zeros_like(f) if h is None else h.double()
+    want = f * s + i * v
+    # the slope of either gate is at most 1/4; the gates themselves as in gated_ref, |u| may exceed XMAX by little
+    mag = f * s.abs() + i * v.abs()
+    err = 0.25 * e[:, 0] * s.abs() + i * e[:, -1] + 0.25 * (e[:, 0] if G == 2 else e[:, 1]) * v.abs() + (ref.GATE + 8) * ref.EPS * mag
+    return want, err
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("G,heads,dh,group", [(2, 1, 64, 32), (3, 2, 64, 64), (2, 1, 640, 128), (3, 1, 512, 32)])
+@pytest.mark.parametrize("B", [1, 3, 16, 20, 48, 64, 70, 129])
+def test_step(P, B, G, heads, dh, group, dtype):
+    gen = torch.Generator().manual_seed(B + dh)
+    codes, scales = ref.quantise(weights(G, heads, dh, seed=B), group)
+    x = torch.randn(B, heads * dh, generator=gen).to(dtype)
+    bias = torch.randn(G, heads * dh, generator=gen) if B % 2 else None
+    h = torch.randn(B, heads * dh, generator=gen) if B != 3 else None
+    Wq = P.pack_projection(codes.cuda(), scales.cuda(), n_heads=heads)
+    y, nxt = P.gated_layer_step(x.cuda(), Wq, None if h is None else h.cuda(), None if bias is None else bias.cuda())
+    want, err = step_reference(x, ref.values(codes, scales), scales, h, bias, heads, G)
+    ref.check(nxt, want, err, "h_next")
+    ref.check(y, want, err, "y")
+    assert torch.equal(y, nxt.to(dtype))
+    if h is not None:                            # in place
+        state = h.cuda()
+        y2, n2 = P.gated_layer_step(x.cuda(), Wq, state, None if bias is None else bias.cuda(), out=(torch.empty_like(y), state))
+        assert n2.data_ptr() == state.data_ptr() and torch.equal(n2, nxt) and torch.equal(y2, y)
+
+
+def test_step_is_captured(P):
+    Wq = P.quantize_projection(weights(2, 1, 256, seed=8).cuda())
+    x, h = torch.randn(4, 256, device="cuda"), torch.randn(4, 256, device="cuda")
+    y = torch.empty_like(x)
+    P.gated_layer_step(x, Wq, h)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        P.gated_layer_step(x, Wq, h, out=(y, h))
+    for _ in range(4):
+        before = h.clone()
+        x.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        e_y, e_h = P.gated_layer_step(x, Wq, before)
+        assert torch.equal(y, e_y) and torch.equal(h, e_h)
+
+
+# ---------------------------------------------------------------- together
+def test_a_layer_from_training_to_serving(P):
+    """A training step, the weights to 4 bits, a padded batch of prompts, then tokens: against the plain form of the 4-bit
+    layer over whole sequences.  bf16; few rows, so that prompt and tokens see the same weights."""
+    gen = torch.Generator().manual_seed(91)
+    B, L, T, H, heads, G = 3, 20, 6, 256, 2, 3
+    x = torch.randn(B, L + T, H, generator=gen).to(torch.bfloat16)
+    W = weights(G, heads, H // heads, seed=91).cuda().requires_grad_()
+    bias = torch.randn(G, H, generator=gen).cuda().requires_grad_()
+    h, _ = P.gated_layer(x.cuda(), W, bias, n_heads=heads)
+    gW, gb = torch.autograd.grad(h.float().square().mean(), (W, bias))
+    W, bias = (W - 0.1 * gW).detach(), (bias - 0.1 * gb).detach()
+    Wq = P.quantize_projection(W, n_heads=heads, group=64)
+    lengths = [20, 7, 0]
+    u = P.input_projection_q4(x[:, :L].contiguous().cuda(), Wq, bias)
+    out, state, _ = P.gated_forward(u, lengths=torch.tensor(lengths, dtype=torch.int32, device="cuda"))
+    got = [state.clone()]
+    tokens = []
+    for t in range(T):
+        y, state = P.gated_layer_step(x[:, L + t].contiguous().cuda(), Wq, state, bias)
+        tokens.append(y)
+        got.append(state)
+    V = P.dequantize_projection(Wq).cpu().double()
+    for k, n in enumerate(lengths):
+        seq = torch.cat([x[k, :n], x[k, L:]])
+        want, _, _, _ = ref.forward(ref.project(seq, V, bias, heads).view(1, n + T, G, H))
+        want = want[0]
+        # pre-activations of the prompt are rounded to bf16 once: half a step of |u| <= 8 each, through slopes of at most 1/4 and
+        # memories of a few steps
+        for t in range(T):
+            assert ((tokens[t][k].double().cpu() - want[n + t]).abs() <= 0.1).all()
+            assert ((got[t + 1][k].double().cpu() - want[n + t]).abs() <= 0.1).all()
+        if n == 0:
+            assert (got[0][k] == 0).all()
+            for t in range(T):                   # tokens alone are exact to fp32
+                assert ((got[t + 1][k].double().cpu() - want[t]).abs() <= 1e-4).all()
+
+
+def test_the_decode_of_a_nonlinear_cell(P):
+    """4-bit pre-activations go where the projection's go: one token of the GRU."""
+    gen = torch.Generator().manual_seed(95)
+    Wq = P.quantize_projection(weights(3, 1, 128, seed=95).cuda(), group=32)
+    x = torch.randn(4, 1, 128, generator=gen).cuda()
+    params = torch.zeros(2, 3, 128, device="cuda")
+    params[0].uniform_(-0.9, 0.9)
+    h0 = torch.randn(4, 1, 128, device="cuda")
+    u = P.input_projection_q4(x, Wq)
+    h, iters, _ = P.forward("gru_diag", params, u, h0, tol=1e-5)
+    a, p, s = u.double()[:, 0], params.double(), h0.double()[:, 0]
+    z, r = torch.sigmoid(p[0, 0] * s + a[:, 0]), torch.sigmoid(p[0, 1] * s + a[:, 1])
+    want = (1 - z) * s + z * torch.tanh(p[0, 2] * r * s + a[:, 2])
+    assert iters.cpu()[1] == 0 and ((h[:, 0, 0].double() - want).abs() <= 1e-5).all()
+
+
+# ---------------------------------------------------------------- refusals
+def test_refusals(P):
+    W = weights(2, 2, 128, seed=1).cuda()
+    Wq = P.quantize_projection(W, n_heads=2, group=64)
+    codes, scales = torch.zeros(2, 256, 128, dtype=torch.int8, device="cuda"), torch.ones(2, 256, 2, dtype=torch.bfloat16, device="cuda")
+    x = torch.zeros(2, 3, 256, device="cuda")
+    row = torch.zeros(2, 256, device="cuda")
+    bad = [
+        (ValueError, lambda: P.quantize_projection(W.cpu())),
+        (ValueError, lambda: P.quantize_projection(W.bfloat16(), n_heads=2)),
+        (ValueError, lambda: P.quantize_projection(W, n_heads=1)),
+        (ValueError, lambda: P.quantize_projection(W, n_heads=0)),
+        (ValueError, lambda: P.quantize_projection(W, n_heads=2, group=48)),
+        (ValueError, lambda: P.quantize_projection(W, n_heads=2, group=256)),
+        (ValueError, lambda: P.quantize_projection(W.transpose(0, 1), n_heads=2)),
+        (ValueError, lambda: P.quantize_projection(torch.zeros(1, 96, 96, device="cuda"))),
+        (ValueError, lambda: P.quantize_projection(torch.zeros(1, 64, 64, device="cuda"), group=128)),
+        (ValueError, lambda: P.quantize_projection(torch.zeros(9, 64, 64, device="cuda"))),
+        (ValueError, lambda: P.pack_projection(codes, scales[:, :, :1].contiguous().float(), n_heads=2)),
+        (ValueError, lambda: P.pack_projection(codes, scales.cpu(), n_heads=2)),
+        (ValueError, lambda: P.pack_projection(codes.int(), scales, n_heads=2)),
+        (ValueError, lambda: P.pack_projection(codes, scales[0], n_heads=2)),
+        (ValueError, lambda: P.input_projection_q4(x.cpu(), Wq)),
+        (ValueError, lambda: P.input_projection_q4(x[0], Wq)),
+        (ValueError, lambda: P.input_projection_q4(x[:, :, :128].contiguous(), Wq)),
+        (ValueError, lambda: P.input_projection_q4(x, Wq, torch.zeros(3, 256, device="cuda"))),
+        (KeyError, lambda: P.input_projection_q4(x.half(), Wq)),
+        (RuntimeError, lambda: P.input_projection_q4(x[:0], Wq)),
+        (RuntimeError, lambda: P.input_projection_q4(torch.zeros(1, 100, 256, device="cuda", dtype=torch.bfloat16), Wq,
+                                                     workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))),
+        (ValueError, lambda: P.gated_layer_step(x, Wq)),
+        (ValueError, lambda: P.gated_layer_step(row, Wq, row.bfloat16())),
+        (ValueError, lambda: P.gated_layer_step(row, Wq, row[:1])),
+        (ValueError, lambda: P.gated_layer_step(row, P.quantize_projection(weights(1, 2, 128, seed=1).cuda(), n_heads=2))),
+        (RuntimeError, lambda: P.gated_layer_step(row[:0], Wq)),
+    ]
+    for k, (error, call) in enumerate(bad):
+        with pytest.raises(error):
+            call()
+            print("case", k)
+    # x at an address that its 16-byte loads do not allow
+    flat = torch.zeros(2 * 256 + 1, device="cuda")
+    with pytest.raises(RuntimeError):
+        P.gated_layer_step(flat[1:].view(2, 256), Wq)
