@@ -210,7 +210,7 @@ int pararnn_set_fused_tail(int enable);
  * that memory (it is not freed and allocated anew, not used as scratch by
  * anybody else, not shared by calls that run at the same time).  pararnn_forward
  * and pararnn_backward of the diagonal and block-diagonal cells (user cells
- * included) then note, per device and address, the layout of the last call and
+ * included), pararnn_gated_forward and pararnn_gated_backward then note, per device and address, the layout of the last call and
  * a call number, put the number into the tags of the carry records, and skip
  * the clearing of the records when the next call on that workspace has the same
  * layout: records of the earlier call carry another number and read as empty.
@@ -459,7 +459,9 @@ int pararnn_input_projection_backward(int dtype, const void *x, const float *Wx,
  *                   when no gradient is wanted.  The backward call takes them in place of h0
  *                   and h: it recomputes the fp32 states between them.
  *   workspace       pararnn_gated_workspace_bytes() bytes (0 on invalid arguments), for either
- *                   direction, 256-byte aligned, no initialisation
+ *                   direction, 256-byte aligned, no initialisation; 256 bytes: not used, may be NULL.
+ *                   Under a promise (pararnn_workspace_keep, pararnn_set_workspace_reuse) it is
+ *                   not cleared again, calls of either direction in any order
  * Gradients, with lam_l the gradient of h_l: lam_l = g_l + f_{l+1} lam_{l+1} (+ dL_dlast behind the
  * last step), dv = lam i, du_i = lam v i (1 - i), du_f = lam h_{l-1} f (1 - f), for G = 2
  * du_f = lam (h_{l-1} - v) f (1 - f), dL_dh0 = f_1 lam_1.

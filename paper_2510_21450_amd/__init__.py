@@ -21,8 +21,8 @@ __all__ = _AUTOGRAD + _BINDING
 
 
 def __getattr__(name):
-    if name in _BINDING:
-        return getattr(importlib.import_module(".binding", __name__), name)
-    if name in _AUTOGRAD:
-        return getattr(importlib.import_module(".autograd", __name__), name)
-    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    module = ".binding" if name in _BINDING else ".autograd" if name in _AUTOGRAD else None
+    if module is None:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    value = globals()[name] = getattr(importlib.import_module(module, __name__), name)      # found here from now on
+    return value

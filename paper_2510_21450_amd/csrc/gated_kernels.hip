@@ -26,6 +26,9 @@ namespace {
 
 constexpr int kTT = 128;                 // steps of a tile
 constexpr int kCW = 64;                  // channels of a tile
+constexpr int kQueues = 16;              // counters that hand out tiles, kQueuePitch words apart (a line each)
+constexpr int kQueuePitch = 32;
+constexpr int kWaves = 8;                // of a tile's workgroup
 constexpr int kShort = 16;               // sequences up to this length: a thread walks them
 
 // ------------------------------------------------------------------ accesses
@@ -50,7 +53,10 @@ template <typename T, int VEC> __device__ __forceinline__ Raw<T, VEC> load_raw_a
     constexpr int BYTES = sizeof(T) * VEC;
     if constexpr (BYTES == 2) x.w[0] = __builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0);
     else if constexpr (BYTES == 4) x.w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0);
-    else {
+    else if constexpr (BYTES == 8) {
+        const u2v v = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+        x.w[0] = v.x; x.w[1] = v.y;
+    } else {
         static_assert(BYTES == 16, "");
         const u4v v = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
         x.w[0] = v.x; x.w[1] = v.y; x.w[2] = v.z; x.w[3] = v.w;
@@ -72,6 +78,7 @@ template <typename T, int VEC> __device__ __forceinline__ void store_at(buf_rsrc
     }
     if constexpr (BYTES == 2) __builtin_amdgcn_raw_buffer_store_b16((unsigned short)w[0], r, off, 0, 0);
     else if constexpr (BYTES == 4) __builtin_amdgcn_raw_buffer_store_b32(w[0], r, off, 0, 0);
+    else if constexpr (BYTES == 8) __builtin_amdgcn_raw_buffer_store_b64(u2v{w[0], w[1]}, r, off, 0, 0);
     else {
         const u4v v = {w[0], w[1], w[2], w[3]};
         __builtin_amdgcn_raw_buffer_store_b128(v, r, off, 0, 0);
@@ -81,7 +88,17 @@ __device__ __forceinline__ buf_rsrc rsrc_of(const void *base, unsigned int bytes
 {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, bytes, 0x27000);
 }
-constexpr unsigned int kOutside = 0xfffffff0u;        // an offset behind every bound (tensors of a tile stay below 2^32 - 256 bytes)
+constexpr unsigned int kOutside = 0x80000000u;        // an offset behind every bound, with any row's added (a tile's rows stay below 2^31 bytes)
+// Registers are what the number of waves hangs on, so values are held to where they are formed:
+// unknown(): a value the compiler knows nothing about.  Offsets of stores are formed where the stores are, not kept (one for each row
+// and gate) from the loads of the same rows on, and packed elements are unpacked again at their second use.
+// formed(): what is computed before this point is not put off behind it, with all its operands alive until then.
+__device__ __forceinline__ unsigned int unknown(unsigned int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+__device__ __forceinline__ void formed(float &x) { asm volatile("" : "+v"(x)); }
 
 // ------------------------------------------------------------------ gates
 // f = sig(x) and 1 - f, the latter as e^-x f: exact where f rounds to 1.  e^-x is held below 2^126, so that its product with f is
@@ -107,47 +124,70 @@ __device__ __forceinline__ word_t get(const word_t *p) { return __hip_atomic_loa
 __device__ __forceinline__ bool has_tag(word_t w, unsigned int tag) { return (unsigned int)(w >> 32) == tag; }
 __device__ __forceinline__ float value(word_t w) { return __uint_as_float((unsigned int)w); }
 
-// The value that enters tile lt from its neighbours in direction dir, for one channel a lane, by a whole wave: the state behind
-// the nearest tile that has one, carried through the maps of those in between in the order and with the roundings those tiles
-// themselves use, so that the result has the same bits whichever tile that is.  U tiles are asked together, one trip to memory.
+// The values that enter tile lt from its neighbours in direction dir: the state behind the nearest tile that has one, carried through
+// the maps of those in between in the order and with the roundings those tiles themselves use, so that the result has the same
+// bits whichever tile that is.  The whole workgroup looks: wave w at the tile w + 1 steps away, a lane for each channel, so that W
+// tiles are asked in one trip to memory and no wave keeps more than one of them in registers.  Returns the number of maps
+// between (the tiles found are in LDS then, carry_of() puts them together), or -1 when the wait ran out.
 // Tiles are numbered by a ticket in the order of their chain: every tile in front has been started by a workgroup that never
 // waits for this one, and the first of a chain publishes its state without waiting, so the wait ends.  A bound on the polls
 // ends it whatever happens; the result is then NaN.
-__device__ __forceinline__ float look_back(const word_t *rec, int dir, int lt, int n_lt, bool active, unsigned int tag_agg,
-                                           unsigned int tag_inc, unsigned int spin_limit)
+template <int W, int LK> struct Seen {          // LK: tiles that a wave looks at in one trip
+    float a[2][W * LK][kCW], s[2][W * LK][kCW];        // s: of a map, or the state behind the tile
+    int what[2][W * LK];                                  // 2: a state, 1: a map, 0: neither yet
+};
+template <int W, int LK>
+__device__ __forceinline__ int look_back(Seen<W, LK> &seen, const word_t *rec, int dir, int lt, int n_lt, bool active,
+                                                          unsigned int tag, unsigned int spin_limit, int *parity)
 {
-    constexpr int U = 8;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (unsigned int spins = 0; spins < spin_limit; ++spins) {
-        word_t a[U], s[U], x[U];
+        const int b = spins & 1;
+        word_t x[LK], a[LK], s[LK];
+        bool exists[LK];
 #pragma unroll
-        for (int q = 0; q < U; ++q) {
-            const int j = lt + (q + 1) * dir;
-            const word_t *p = rec + (long long)(j >= 0 && j < n_lt ? j - lt : dir) * 3 * kCW;      // lt + dir exists
-            x[q] = get(p + 2 * kCW);
-            if (q < U - 1) { a[q] = get(p); s[q] = get(p + kCW); }
+        for (int k = 0; k < LK; ++k) {
+            const int j = lt + (w * LK + k + 1) * dir;
+            exists[k] = j >= 0 && j < n_lt;
+            const word_t *p = rec + (long long)(exists[k] ? j - lt : dir) * 3 * kCW + lane;      // lt + dir exists
+            x[k] = get(p + 2 * kCW);
+            a[k] = get(p);
+            s[k] = get(p + kCW);
         }
-        int found = -1;
-        bool reachable = true;
 #pragma unroll
-        for (int q = 0; q < U; ++q) {
-            const int j = lt + (q + 1) * dir;
-            if (found < 0 && reachable && j >= 0 && j < n_lt) {
-                if (__all(!active || has_tag(x[q], tag_inc))) found = q;
-                else reachable = q < U - 1 && __all(!active || (has_tag(a[q], tag_agg) && has_tag(s[q], tag_agg)));
-            }
+        for (int k = 0; k < LK; ++k) {
+            int what = 0;
+            if (exists[k]) what = __all(!active || has_tag(x[k], tag + 2)) ? 2 : __all(!active || (has_tag(a[k], tag + 1) && has_tag(s[k], tag + 1))) ? 1 : 0;
+            seen.a[b][w * LK + k][lane] = value(a[k]);
+            seen.s[b][w * LK + k][lane] = what == 2 ? value(x[k]) : value(s[k]);
+            if (lane == 0) seen.what[b][w * LK + k] = what;
         }
-        if (found >= 0) {
-            float v = 0.0f;
-#pragma unroll
-            for (int q = U - 1; q >= 0; --q) {
-                if (q == found) v = value(x[q]);
-                else if (q < U - 1 && q < found) v = fmaf(value(a[q]), v, value(s[q]));
-            }
-            return active ? v : 0.0f;
+        __syncthreads();
+        // (two buffers: a wave that goes on writes the other one, and is held by the next barrier until all have read this one)
+        static_assert(W * LK <= 64, "");
+        const int what = seen.what[b][lane % (W * LK)];
+        const unsigned long long states = __ballot(what == 2), gaps = __ballot(what == 0);
+        if (states && (!gaps || __builtin_ctzll(states) < __builtin_ctzll(gaps))) {
+            *parity = b;
+            return __builtin_ctzll(states);
         }
         __builtin_amdgcn_s_sleep(1);
     }
-    return __uint_as_float(0x7fc00000u);
+    return -1;
+}
+// N channels from c on: what the look found
+template <int N, int W, int LK> __device__ __forceinline__ void carry_of(const Seen<W, LK> &seen, int found, int parity, int c, float (&v)[N])
+{
+    if (found < 0) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = __uint_as_float(0x7fc00000u);
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = seen.s[parity][found][c + k];
+    for (int q = found - 1; q >= 0; --q)
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = fmaf(seen.a[parity][q][c + k], v[k], seen.s[parity][q][c + k]);
 }
 
 struct GatedArgs {
@@ -165,7 +205,7 @@ struct GatedArgs {
     word_t *rec;                  // [chain][tile][3][kCW]
     unsigned int tag;             // of this call: aggregates carry tag + 1, states tag + 2
     unsigned int spin_limit;
-    int B, L, H, n_lt, groups, chains;
+    int B, L, H, n_lt, groups, chains, queues;
 };
 
 // Where a workgroup's tile lies.
@@ -174,17 +214,33 @@ struct Place {
     int rows, rows_all;           // valid steps, and all steps, of the tile
 };
 
+// Chains are shared out among up to kQueues queues, neighbours to the same one: a queue hands out the tiles of its chains with a
+// ticket, along time first for none of them (all chains' first tiles, then all second ones).  One counter for all tiles
+// bounds a launch: its atomics take 12.5 ns each, 1.7 ms for 131072 tiles that move 6.4 GB.  Queue q's workgroups are
+// launched q, q + kQueues, ..., which are on one XCD, so that a line shared by two groups of channels is in its L2.
+// The last workgroup of a queue leaves the counter at zero for the next call.
 template <bool LOOK, bool REVERSE> __device__ __forceinline__ Place place_of(const GatedArgs &a, int *s_id)
 {
-    int id = (int)blockIdx.x;
-    if constexpr (LOOK) {
-        if (threadIdx.x == 0) *s_id = (int)atomicAdd(a.ticket, 1u);
-        __syncthreads();
-        id = __builtin_amdgcn_readfirstlane(*s_id);
-    }
     Place p;
-    p.lt = LOOK ? id / a.chains : 0;
-    p.chain = id - p.lt * a.chains;
+    if constexpr (LOOK) {
+        const int each = a.chains / a.queues, more = a.chains - each * a.queues;      // the first `more` queues have one chain more
+        const int even = a.queues * each * a.n_lt, block = (int)blockIdx.x;
+        const int q = block < even ? block % a.queues : (block - even) % more;
+        const int n = each + (q < more), first = q * each + (q < more ? q : more);
+        if (threadIdx.x == 0) {
+            unsigned int *ticket = a.ticket + q * kQueuePitch;
+            const unsigned int t = atomicAdd(ticket, 1u);
+            if (t + 1 == (unsigned int)n * (unsigned int)a.n_lt) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            *s_id = (int)t;
+        }
+        __syncthreads();
+        const int id = __builtin_amdgcn_readfirstlane(*s_id);
+        p.lt = id / n;
+        p.chain = first + id - p.lt * n;
+    } else {
+        p.lt = 0;
+        p.chain = (int)blockIdx.x;
+    }
     if (REVERSE) p.lt = a.n_lt - 1 - p.lt;
     p.b = p.chain / a.groups;
     p.grp = p.chain - p.b * a.groups;
@@ -197,6 +253,13 @@ template <bool LOOK, bool REVERSE> __device__ __forceinline__ Place place_of(con
     p.rows = p.rows < 0 ? 0 : p.rows > kTT ? kTT : p.rows;
     p.rows_all = a.L - p.lt * kTT;
     p.rows_all = p.rows_all > kTT ? kTT : p.rows_all;
+    // the same in all lanes, which the compiler does not see through the divisions: resources built from them would be used lane by lane
+    p.b = __builtin_amdgcn_readfirstlane(p.b);
+    p.grp = __builtin_amdgcn_readfirstlane(p.grp);
+    p.lt = __builtin_amdgcn_readfirstlane(p.lt);
+    p.chain = __builtin_amdgcn_readfirstlane(p.chain);
+    p.rows = __builtin_amdgcn_readfirstlane(p.rows);
+    p.rows_all = __builtin_amdgcn_readfirstlane(p.rows_all);
     return p;
 }
 
@@ -206,18 +269,22 @@ __device__ __forceinline__ unsigned int extent(int n, unsigned int row_bytes, un
     return n > 0 ? (unsigned int)n * row_bytes - first : 0u;
 }
 
-template <typename T, int G, int VEC, int W, int C, bool LOOK>
+template <typename T, int G, int VEC, int W, int C, int LK>
 __global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a)
 {
     constexpr int LPR = kCW / VEC, SEG = 64 / LPR;
     static_assert(W * SEG * C == kTT, "");
     __shared__ float s_a[W][kCW], s_s[W][kCW], s_in[kCW];
+    constexpr bool LOOK = LK > 0;
+    __shared__ Seen<LOOK ? W : 1, LOOK ? LK : 1> s_seen;
     __shared__ int s_id;
     const Place p = place_of<LOOK, false>(a, &s_id);
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, sg = lane / LPR, c0 = (lane % LPR) * VEC;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sg = lane / LPR, c0 = (lane % LPR) * VEC;
     const int t0 = (w * SEG + sg) * C;
     const unsigned int es = sizeof(T), H = (unsigned int)a.H, first = (unsigned int)p.grp * kCW;
     const bool active = first + c0 < H;
+    const unsigned int row_bytes = H * es, at_h = (active ? c0 * es : kOutside) + (unsigned int)t0 * row_bytes;
+    const unsigned int at_u = at_h + (unsigned int)t0 * (G - 1) * row_bytes;
 
     const size_t row = (size_t)p.b * a.L + (size_t)p.lt * kTT;
     const buf_rsrc ru = rsrc_of(static_cast<const T *>(a.u) + row * G * H + first, extent(p.rows, G * H * es, first * es));
@@ -226,14 +293,18 @@ __global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a
     for (int j = 0; j < C; ++j)
 #pragma unroll
         for (int g = 0; g < G; ++g)
-            raw[j][g] = load_raw_at<T, VEC>(ru, active ? (((unsigned int)(t0 + j) * G + g) * H + c0) * es : kOutside);
+            raw[j][g] = load_raw_at<T, VEC>(ru, at_u + (unsigned int)(j * G + g) * row_bytes);
+
+    const unsigned int ch = first + lane;                    // wave 0: a lane for each channel of the tile
+    const bool act = ch < H;
+    const float in0 = w == 0 && p.lt == 0 && act && a.h0 ? a.h0[(size_t)p.b * H + ch] : 0.0f;
 
     float f[C][VEC], b[C][VEC], A[VEC], S[VEC];
 #pragma unroll
     for (int k = 0; k < VEC; ++k) { A[k] = 1.0f; S[k] = 0.0f; }
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-        const bool valid = t0 + j < p.rows;
+        const bool valid = t0 < p.rows - j;
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
             float ff, om, i;
@@ -252,10 +323,8 @@ __global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
             const float a1 = __shfl_up(A[k], d, 64), s1 = __shfl_up(S[k], d, 64);
-            if (lane >= d) {
-                S[k] = fmaf(A[k], s1, S[k]);
-                A[k] *= a1;
-            }
+            S[k] = fmaf(A[k], lane >= d ? s1 : 0.0f, S[k]);
+            A[k] *= lane >= d ? a1 : 1.0f;
         }
     if (sg == SEG - 1)
 #pragma unroll
@@ -271,64 +340,75 @@ __global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a
 #pragma unroll
         for (int k = 0; k < VEC; ++k) { A[k] = 1.0f; S[k] = 0.0f; }
     }
+    if (w == 0) s_in[lane] = in0;
     __syncthreads();
-    if (w == 0) {                                            // a lane for each channel of the tile
-        const unsigned int ch = first + lane;
-        const bool act = ch < H;
-        float ta = 1.0f, ts = 0.0f;
-#pragma unroll
-        for (int q = 0; q < W; ++q) { ts = fmaf(s_a[q][lane], ts, s_s[q][lane]); ta *= s_a[q][lane]; }
-        float in = 0.0f;
-        word_t *rec = a.rec + ((size_t)p.chain * a.n_lt + p.lt) * (3 * kCW) + lane;
-        if (!LOOK || p.lt == 0) {
-            if (a.h0 && act) in = a.h0[(size_t)p.b * H + ch];
-        } else {
-            if (act && p.lt + 1 < a.n_lt) { put(rec, ta, a.tag + 1); put(rec + kCW, ts, a.tag + 1); }
-            in = look_back(rec, -1, p.lt, a.n_lt, act, a.tag + 1, a.tag + 2, a.spin_limit);
-        }
-        const float out = fmaf(ta, in, ts);
-        if (LOOK && act && p.lt + 1 < a.n_lt) put(rec + 2 * kCW, out, a.tag + 2);
-        s_in[lane] = in;
-        if (a.ckpt && act) a.ckpt[((size_t)p.b * a.n_lt + p.lt) * H + ch] = in;
-        if (a.last && act && p.lt + 1 == a.n_lt) a.last[(size_t)p.b * H + ch] = out;
-    }
-    // this wave's place among the waves, while the first one waits
+    // this wave's place among the waves
     float x[VEC], pa[VEC], ps[VEC];
 #pragma unroll
     for (int k = 0; k < VEC; ++k) { pa[k] = 1.0f; ps[k] = 0.0f; }
     for (int q = 0; q < w; ++q)
 #pragma unroll
         for (int k = 0; k < VEC; ++k) { ps[k] = fmaf(s_a[q][c0 + k], ps[k], s_s[q][c0 + k]); pa[k] *= s_a[q][c0 + k]; }
-    __syncthreads();
+    const bool more = LOOK && p.lt + 1 < a.n_lt;
+    word_t *rec = a.rec + ((size_t)p.chain * a.n_lt + p.lt) * (3 * kCW);
+    float ta = 1.0f, ts = 0.0f;
+    if (w == 0) {
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) x[k] = fmaf(A[k], fmaf(pa[k], s_in[c0 + k], ps[k]), S[k]);
+        for (int q = 0; q < W; ++q) { ts = fmaf(s_a[q][lane], ts, s_s[q][lane]); ta *= s_a[q][lane]; }
+        if (more && act && p.lt > 0) { put(rec + lane, ta, a.tag + 1); put(rec + kCW + lane, ts, a.tag + 1); }
+    }
+    int found = -1, parity = 0;
+    if constexpr (LOOK)
+        if (p.lt > 0) found = look_back(s_seen, rec, -1, p.lt, a.n_lt, act, a.tag, a.spin_limit, &parity);
+    auto entering = [&](int c, auto &v) {                    // the state in front of the tile
+        if constexpr (LOOK)
+            if (p.lt > 0) return carry_of(s_seen, found, parity, c, v);
+#pragma unroll
+        for (int k = 0; k < (int)(sizeof(v) / sizeof(v[0])); ++k) v[k] = s_in[c + k];
+    };
+    if (w == 0 && act) {
+        float in1[1];
+        entering(lane, in1);
+        const float in = in1[0], out = fmaf(ta, in, ts);
+        if (more) put(rec + 2 * kCW + lane, out, a.tag + 2);
+        if (a.ckpt) a.ckpt[((size_t)p.b * a.n_lt + p.lt) * H + ch] = in;
+        if (a.last && p.lt + 1 == a.n_lt) a.last[(size_t)p.b * H + ch] = out;      // (may be h0: read before the first state was published)
+    }
+    entering(c0, x);
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) x[k] = fmaf(A[k], fmaf(pa[k], x[k], ps[k]), S[k]);
 
+    const unsigned int at_out = unknown(at_h);
     const buf_rsrc rh = rsrc_of(static_cast<T *>(a.h) + row * H + first, extent(p.rows_all, H * es, first * es));
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-        const bool valid = t0 + j < p.rows;
+        const bool valid = t0 < p.rows - j;
         float o[VEC];
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
             x[k] = fmaf(f[j][k], x[k], b[j][k]);
             o[k] = valid ? x[k] : 0.0f;
         }
-        store_at<T, VEC>(rh, active ? ((unsigned int)(t0 + j) * H + c0) * es : kOutside, o);
+        store_at<T, VEC>(rh, at_out + (unsigned int)j * row_bytes, o);
     }
 }
 
-template <typename T, int G, int VEC, int W, int C, bool LOOK>
-__global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedArgs a)
+template <typename T, int G, int VEC, int W, int C, int LK>
+__global__ __launch_bounds__(64 * W, 4) void gated_backward_kernel(const GatedArgs a)
 {
     constexpr int LPR = kCW / VEC, SEG = 64 / LPR;
     static_assert(W * SEG * C == kTT, "");
     __shared__ float s_a[W][kCW], s_s[W][kCW], s_m[W][kCW], s_in[kCW];
+    constexpr bool LOOK = LK > 0;
+    __shared__ Seen<LOOK ? W : 1, LOOK ? LK : 1> s_seen;
     __shared__ int s_id;
     const Place p = place_of<LOOK, true>(a, &s_id);
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, sg = lane / LPR, c0 = (lane % LPR) * VEC;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sg = lane / LPR, c0 = (lane % LPR) * VEC;
     const int t0 = (w * SEG + sg) * C;
     const unsigned int es = sizeof(T), H = (unsigned int)a.H, first = (unsigned int)p.grp * kCW;
     const bool active = first + c0 < H;
+    const unsigned int row_bytes = H * es, at_h = (active ? c0 * es : kOutside) + (unsigned int)t0 * row_bytes;
+    const unsigned int at_u = at_h + (unsigned int)t0 * (G - 1) * row_bytes;
 
     const size_t row = (size_t)p.b * a.L + (size_t)p.lt * kTT;
     const buf_rsrc ru = rsrc_of(static_cast<const T *>(a.u) + row * G * H + first, extent(p.rows, G * H * es, first * es));
@@ -338,33 +418,57 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedArgs 
     for (int j = 0; j < C; ++j) {
 #pragma unroll
         for (int g = 0; g < G; ++g)
-            raw[j][g] = load_raw_at<T, VEC>(ru, active ? (((unsigned int)(t0 + j) * G + g) * H + c0) * es : kOutside);
-        rawg[j] = load_raw_at<T, VEC>(rg, active ? ((unsigned int)(t0 + j) * H + c0) * es : kOutside);
+            raw[j][g] = load_raw_at<T, VEC>(ru, at_u + (unsigned int)(j * G + g) * row_bytes);
+        rawg[j] = load_raw_at<T, VEC>(rg, at_h + (unsigned int)j * row_bytes);
     }
+    const unsigned int ch = first + lane;                    // wave 0: a lane for each channel of the tile
+    const bool act = ch < H;
+    const float in0 = w == 0 && p.lt + 1 == a.n_lt && act && a.dlast ? a.dlast[(size_t)p.b * H + ch] : 0.0f;
     float before[VEC];                                       // the state in front of the tile
 #pragma unroll
     for (int k = 0; k < VEC; ++k) before[k] = active ? a.ckpt[((size_t)p.b * a.n_lt + p.lt) * H + first + c0 + k] : 0.0f;
 
-    float f[C][VEC], om[C][VEC], i[C][VEC], A[VEC], S[VEC], M[VEC], RA[VEC];
+    // cf, ci and i: what lam is multiplied by for the gradients of the gates and of v (cf first without the state)
+    float f[C][VEC], i[C][VEC], cf[C][VEC], ci[G == 3 ? C : 1][VEC], A[VEC], S[VEC], M[VEC], RA[VEC];
 #pragma unroll
     for (int k = 0; k < VEC; ++k) { A[k] = 1.0f; S[k] = M[k] = 0.0f; }
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-        const bool valid = t0 + j < p.rows;
+        const bool valid = t0 < p.rows - j;
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
-            sigmoid2(raw[j][0].at(k), &f[j][k], &om[j][k]);
-            if (!valid) { f[j][k] = 1.0f; om[j][k] = 0.0f; }
-            i[j][k] = om[j][k];
-            if constexpr (G == 3) i[j][k] = valid ? fast_sigmoid(raw[j][1].at(k)) : 0.0f;
+            const float v = raw[j][G - 1].at(k);             // (zero behind the valid steps)
+            float ff, om;
+            sigmoid2(raw[j][0].at(k), &ff, &om);
+            if constexpr (G == 3) {
+                float ii, oi;
+                sigmoid2(raw[j][1].at(k), &ii, &oi);
+                ci[j][k] = v * (ii * oi);
+                formed(ci[j][k]);
+                i[j][k] = ii;
+            } else {
+                i[j][k] = om;
+            }
+            cf[j][k] = ff * om;
+            formed(cf[j][k]);
+            f[j][k] = valid ? ff : 1.0f;
             A[k] *= f[j][k];
-            S[k] = fmaf(f[j][k], S[k], i[j][k] * raw[j][G - 1].at(k));       // behind the valid steps v is loaded as zero
+            S[k] = fmaf(f[j][k], S[k], i[j][k] * v);
         }
     }
 #pragma unroll
     for (int j = C - 1; j >= 0; --j)
 #pragma unroll
         for (int k = 0; k < VEC; ++k) M[k] = f[j][k] * (rawg[j].at(k) + M[k]);
+    if constexpr (sizeof(T) == 2)
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+#pragma unroll
+            for (unsigned k = 0; k < sizeof(rawg[j].w) / 4; ++k) {
+                rawg[j].w[k] = unknown(rawg[j].w[k]);
+                raw[j][G - 1].w[k] = unknown(raw[j][G - 1].w[k]);
+            }
+        }
 #pragma unroll
     for (int k = 0; k < VEC; ++k) RA[k] = A[k];
     // along time for the states, against it for the adjoint
@@ -374,14 +478,10 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedArgs 
         for (int k = 0; k < VEC; ++k) {
             const float a1 = __shfl_up(A[k], d, 64), s1 = __shfl_up(S[k], d, 64);
             const float a2 = __shfl_down(RA[k], d, 64), m2 = __shfl_down(M[k], d, 64);
-            if (lane >= d) {
-                S[k] = fmaf(A[k], s1, S[k]);
-                A[k] *= a1;
-            }
-            if (lane + d < 64) {
-                M[k] = fmaf(RA[k], m2, M[k]);
-                RA[k] *= a2;
-            }
+            S[k] = fmaf(A[k], lane >= d ? s1 : 0.0f, S[k]);
+            A[k] *= lane >= d ? a1 : 1.0f;
+            M[k] = fmaf(RA[k], lane + d < 64 ? m2 : 0.0f, M[k]);
+            RA[k] *= lane + d < 64 ? a2 : 1.0f;
         }
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
@@ -402,28 +502,17 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedArgs 
             S[k] = M[k] = 0.0f;
         }
     }
+    if (w == 0) s_in[lane] = in0;
     __syncthreads();
+    const bool more = LOOK && p.lt > 0;
+    word_t *rec = a.rec + ((size_t)p.chain * a.n_lt + p.lt) * (3 * kCW);
+    float ta = 1.0f, tm = 0.0f;
     if (w == 0) {
-        const unsigned int ch = first + lane;
-        const bool act = ch < H;
-        float ta = 1.0f, tm = 0.0f;
 #pragma unroll
         for (int q = W - 1; q >= 0; --q) { tm = fmaf(s_a[q][lane], tm, s_m[q][lane]); ta *= s_a[q][lane]; }
-        float in = 0.0f;
-        word_t *rec = a.rec + ((size_t)p.chain * a.n_lt + p.lt) * (3 * kCW) + lane;
-        if (!LOOK || p.lt + 1 == a.n_lt) {
-            if (a.dlast && act) in = a.dlast[(size_t)p.b * H + ch];
-        } else {
-            if (act && p.lt > 0) { put(rec, ta, a.tag + 1); put(rec + kCW, tm, a.tag + 1); }
-            in = look_back(rec, 1, p.lt, a.n_lt, act, a.tag + 1, a.tag + 2, a.spin_limit);
-        }
-        const float out = fmaf(ta, in, tm);
-        if (LOOK && act && p.lt > 0) put(rec + 2 * kCW, out, a.tag + 2);
-        s_in[lane] = in;
-        if (a.dh0 && act && p.lt == 0) a.dh0[(size_t)p.b * H + ch] = out;
+        if (more && act && p.lt + 1 < a.n_lt) { put(rec + lane, ta, a.tag + 1); put(rec + kCW + lane, tm, a.tag + 1); }
     }
-    // the state in front of this thread's steps, and in front of each of them
-    float hp[C][VEC];
+    // the state in front of each of this thread's steps
     for (int q = 0; q < w; ++q)
 #pragma unroll
         for (int k = 0; k < VEC; ++k) before[k] = fmaf(s_a[q][c0 + k], before[k], s_s[q][c0 + k]);
@@ -433,8 +522,10 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedArgs 
     for (int j = 0; j < C; ++j)
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
-            hp[j][k] = before[k];
-            before[k] = fmaf(f[j][k], before[k], i[j][k] * raw[j][G - 1].at(k));
+            const float v = raw[j][G - 1].at(k);
+            cf[j][k] *= G == 2 ? before[k] - v : before[k];
+            formed(cf[j][k]);
+            before[k] = fmaf(f[j][k], before[k], i[j][k] * v);
         }
     float pa[VEC], pm[VEC];
 #pragma unroll
@@ -442,33 +533,44 @@ __global__ __launch_bounds__(64 * W) void gated_backward_kernel(const GatedArgs 
     for (int q = W - 1; q > w; --q)
 #pragma unroll
         for (int k = 0; k < VEC; ++k) { pm[k] = fmaf(s_a[q][c0 + k], pm[k], s_m[q][c0 + k]); pa[k] *= s_a[q][c0 + k]; }
-    __syncthreads();
-    float m[VEC];
+    int found = -1, parity = 0;
+    if constexpr (LOOK)
+        if (p.lt + 1 < a.n_lt) found = look_back(s_seen, rec, 1, p.lt, a.n_lt, act, a.tag, a.spin_limit, &parity);
+    auto entering = [&](int c, auto &v) {                    // the adjoint behind the tile
+        if constexpr (LOOK)
+            if (p.lt + 1 < a.n_lt) return carry_of(s_seen, found, parity, c, v);
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) m[k] = fmaf(RA[k], fmaf(pa[k], s_in[c0 + k], pm[k]), M[k]);
+        for (int k = 0; k < (int)(sizeof(v) / sizeof(v[0])); ++k) v[k] = s_in[c + k];
+    };
+    if (w == 0 && act) {
+        float in1[1];
+        entering(lane, in1);
+        const float out = fmaf(ta, in1[0], tm);
+        if (more) put(rec + 2 * kCW + lane, out, a.tag + 2);
+        if (a.dh0 && p.lt == 0) a.dh0[(size_t)p.b * H + ch] = out;
+    }
+    float m[VEC];
+    entering(c0, m);
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) m[k] = fmaf(RA[k], fmaf(pa[k], m[k], pm[k]), M[k]);
 
+    const unsigned int at_out = unknown(at_u);
     const buf_rsrc rd = rsrc_of(static_cast<T *>(a.du) + row * G * H + first, extent(p.rows_all, G * H * es, first * es));
 #pragma unroll
     for (int j = C - 1; j >= 0; --j) {
-        const bool valid = t0 + j < p.rows;
+        const bool valid = t0 < p.rows - j;
         float o[G][VEC];
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
-            const float lam = rawg[j].at(k) + m[k], v = raw[j][G - 1].at(k);
-            const float slope = f[j][k] * om[j][k];
+            const float lam = rawg[j].at(k) + m[k];
+            o[0][k] = valid ? lam * cf[j][k] : 0.0f;
+            if constexpr (G == 3) o[1][k] = valid ? lam * ci[j][k] : 0.0f;
             o[G - 1][k] = valid ? lam * i[j][k] : 0.0f;
-            if constexpr (G == 2) {
-                o[0][k] = valid ? lam * (hp[j][k] - v) * slope : 0.0f;
-            } else {
-                // 1 - i from the gate's input: exact where i rounds to 1
-                o[0][k] = valid ? lam * hp[j][k] * slope : 0.0f;
-                o[1][k] = valid ? lam * v * i[j][k] * fast_sigmoid(-raw[j][1].at(k)) : 0.0f;
-            }
             m[k] = f[j][k] * lam;
         }
 #pragma unroll
         for (int g = 0; g < G; ++g)
-            store_at<T, VEC>(rd, active ? (((unsigned int)(t0 + j) * G + g) * H + c0) * es : kOutside, o[g]);
+            store_at<T, VEC>(rd, at_out + (unsigned int)(j * G + g) * row_bytes, o[g]);
     }
 }
 
@@ -541,6 +643,7 @@ __global__ __launch_bounds__(256) void gated_clear_kernel(ulonglong2 *p, size_t 
 }
 
 // ------------------------------------------------------------------ host
+constexpr size_t kCtrl = (size_t)kQueues * kQueuePitch * sizeof(unsigned int);
 struct Shape {
     int n_lt, groups;
     long long chains, tiles;
@@ -554,19 +657,25 @@ bool shape_of(int dtype, int B, int L, int H, int G, Shape *s)
     s->groups = (H + kCW - 1) / kCW;
     s->chains = (long long)B * s->groups;
     s->tiles = s->chains * s->n_lt;
-    s->bytes = 256 + (s->n_lt > 1 ? (size_t)s->tiles * 3 * kCW * sizeof(word_t) : 0);
+    s->bytes = s->n_lt > 1 ? kCtrl + (size_t)s->tiles * 3 * kCW * sizeof(word_t) : 256;
     return true;
 }
 
 // Row offsets of a tile are 32-bit (128 steps x 3 gates x 4 bytes x 2^20 channels), tile numbers too.
-bool size_ok(const Shape &s, int H) { return H <= (1 << 20) && s.tiles < (1ll << 31); }
+bool size_ok(const Shape &s, int H) { return H <= (1 << 20) && s.tiles < (1ll << 31) - 1; }
 
-bool wide_ok(int H, int dtype, std::initializer_list<const void *> ptrs)
+// Whether rows can be taken n elements at a time
+bool rows_of(int n, int H, int dtype, std::initializer_list<const void *> ptrs)
 {
     uintptr_t m = 0;
     for (const void *p : ptrs) m |= (uintptr_t)p;
-    return m % 16 == 0 && H % (dtype == PARARNN_BF16 ? 8 : 4) == 0;
+    return m % ((dtype == PARARNN_BF16 ? 2 : 4) * n) == 0 && H % n == 0;
 }
+
+// A look at 32 tiles in place of 8: few and long chains, whose tiles are on the device all at once and wait for the chain.  4 chains of 512
+// tiles: 92 -> 48 us (forward, 1 x 65536 x 256 bf16), 86 -> 51 (backward); 16 chains of 32 are level, of 64 lose 23 -> 26 and
+// 29 -> 32 (2 x 8192 x 512), 64 of 128 107 -> 120 (2 x 16384 x 2048).
+bool wide_look(const GatedArgs &a) { return a.chains <= 8 && a.n_lt > kWaves; }
 
 hipError_t launch_clear(void *ws, size_t bytes, hipStream_t st)
 {
@@ -576,34 +685,35 @@ hipError_t launch_clear(void *ws, size_t bytes, hipStream_t st)
     return hipGetLastError();
 }
 
-template <typename T, int G> hipError_t launch_forward(const GatedArgs &a, bool wide, unsigned blocks, hipStream_t st)
+// LK: 0 for a single tile along L
+template <typename T, int G, int VEC, int LK> void launch_tiles(const GatedArgs &a, bool backward, hipStream_t st)
 {
-    constexpr int V = 16 / sizeof(T);
-    const bool look = a.n_lt > 1;
-    if (wide) {
-        constexpr int C = kTT / (4 * (64 * V / kCW));
-        if (look) hipLaunchKernelGGL((gated_forward_kernel<T, G, V, 4, C, true>), dim3(blocks), dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((gated_forward_kernel<T, G, V, 4, C, false>), dim3(blocks), dim3(256), 0, st, a);
-    } else {
-        if (look) hipLaunchKernelGGL((gated_forward_kernel<T, G, 1, 8, kTT / 8, true>), dim3(blocks), dim3(512), 0, st, a);
-        else hipLaunchKernelGGL((gated_forward_kernel<T, G, 1, 8, kTT / 8, false>), dim3(blocks), dim3(512), 0, st, a);
-    }
+    constexpr int C = kTT / (kWaves * (64 * VEC / kCW));
+    const dim3 grid((unsigned)a.chains * a.n_lt), block(64 * kWaves);
+    if (backward) hipLaunchKernelGGL((gated_backward_kernel<T, G, VEC, kWaves, C, LK>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((gated_forward_kernel<T, G, VEC, kWaves, C, LK>), grid, block, 0, st, a);
+}
+template <typename T, int G> hipError_t launch_tiles_of(const GatedArgs &a, bool backward, bool pairs, hipStream_t st)
+{
+    const int look = a.n_lt == 1 ? 0 : wide_look(a) ? 4 : 1;
+#define PARARNN_GATED(VEC)                                                    \
+    do {                                                                      \
+        if (look == 0) launch_tiles<T, G, VEC, 0>(a, backward, st);           \
+        else if (look == 1) launch_tiles<T, G, VEC, 1>(a, backward, st);      \
+        else launch_tiles<T, G, VEC, 4>(a, backward, st);                     \
+    } while (0)
+    if (pairs) PARARNN_GATED(2);
+    else PARARNN_GATED(1);
+#undef PARARNN_GATED
     return hipGetLastError();
 }
 
-template <typename T, int G> hipError_t launch_backward(const GatedArgs &a, bool wide, unsigned blocks, hipStream_t st)
+int launch_of(int dtype, int G, const GatedArgs &a, bool backward, bool pairs, hipStream_t st)
 {
-    constexpr int V = 16 / sizeof(T);
-    const bool look = a.n_lt > 1;
-    if (wide) {
-        constexpr int C = kTT / (8 * (64 * V / kCW));
-        if (look) hipLaunchKernelGGL((gated_backward_kernel<T, G, V, 8, C, true>), dim3(blocks), dim3(512), 0, st, a);
-        else hipLaunchKernelGGL((gated_backward_kernel<T, G, V, 8, C, false>), dim3(blocks), dim3(512), 0, st, a);
-    } else {
-        if (look) hipLaunchKernelGGL((gated_backward_kernel<T, G, 1, 8, kTT / 8, true>), dim3(blocks), dim3(512), 0, st, a);
-        else hipLaunchKernelGGL((gated_backward_kernel<T, G, 1, 8, kTT / 8, false>), dim3(blocks), dim3(512), 0, st, a);
-    }
-    return hipGetLastError();
+    const hipError_t e = dtype == PARARNN_BF16
+                             ? (G == 2 ? launch_tiles_of<unsigned short, 2>(a, backward, pairs, st) : launch_tiles_of<unsigned short, 3>(a, backward, pairs, st))
+                             : (G == 2 ? launch_tiles_of<float, 2>(a, backward, pairs, st) : launch_tiles_of<float, 3>(a, backward, pairs, st));
+    return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
 }
 
 template <typename T, int G> hipError_t launch_walk(const GatedArgs &a, bool wide, hipStream_t st)
@@ -614,6 +724,24 @@ template <typename T, int G> hipError_t launch_walk(const GatedArgs &a, bool wid
     if (wide) hipLaunchKernelGGL((gated_walk_kernel<T, G, V>), dim3(blocks), dim3(256), 0, st, a);
     else hipLaunchKernelGGL((gated_walk_kernel<T, G, 1>), dim3(blocks), dim3(256), 0, st, a);
     return hipGetLastError();
+}
+
+// Control block and carry records for the call: cleared, unless the library knows what an earlier call left in this workspace.
+// False: a launch failed.
+bool take_workspace(void *workspace, const Shape &s, GatedArgs *a, hipStream_t st)
+{
+    char *ws = static_cast<char *>(workspace);
+    a->ticket = reinterpret_cast<unsigned int *>(ws);
+    a->rec = reinterpret_cast<word_t *>(ws + kCtrl);
+    a->queues = (int)std::min<long long>(kQueues, s.chains);
+    a->spin_limit = kSpinLimit;
+    // FNV-1a; what the words are used for depends on the numbers of chains and tiles alone
+    unsigned long long sig = 1469598103934665603ull;
+    for (unsigned long long v : {0x6761746564ull, (unsigned long long)s.n_lt, (unsigned long long)s.chains})
+        for (int i = 0; i < 8; ++i) sig = (sig ^ (v >> (8 * i) & 0xff)) * 1099511628211ull;
+    bool fill = true;
+    a->tag = workspace_epoch(workspace, sig ? sig : 1, st, &fill);
+    return !fill || launch_clear(ws, s.bytes, st) == hipSuccess;
 }
 
 bool misaligned(const void *p, size_t n) { return (uintptr_t)p % n != 0; }
@@ -636,32 +764,29 @@ int gated_forward(int dtype, const void *u, const float *h0, const int *lengths,
                   float *h_last, float *checkpoints, void *workspace, size_t workspace_bytes, hipStream_t st)
 {
     Shape s;
-    if (!shape_of(dtype, B, L, H, G, &s) || !u || !h || !workspace || misaligned(workspace, 256)) return PARARNN_INVALID_ARG;
+    if (!shape_of(dtype, B, L, H, G, &s) || !u || !h || (!workspace && s.n_lt > 1) || misaligned(workspace, 256)) return PARARNN_INVALID_ARG;
     const size_t es = dtype == PARARNN_BF16 ? 2 : 4;
     if (misaligned(u, es) || misaligned(h, es) || misaligned(h0, 4) || misaligned(lengths, 4) || misaligned(h_last, 4) ||
         misaligned(checkpoints, 4))
         return PARARNN_INVALID_ARG;
     if (!size_ok(s, H)) return PARARNN_UNSUPPORTED;
-    if (workspace_bytes < s.bytes) return PARARNN_WORKSPACE_TOO_SMALL;
+    if (s.n_lt > 1 && workspace_bytes < s.bytes) return PARARNN_WORKSPACE_TOO_SMALL;
     GatedArgs a = {};
     a.u = u; a.h0 = h0; a.lengths = lengths; a.h = h; a.last = h_last; a.ckpt = checkpoints;
     a.B = B; a.L = L; a.H = H; a.n_lt = s.n_lt; a.groups = s.groups; a.chains = (int)s.chains;
-    const bool wide = wide_ok(H, dtype, {u, h});
     if (L <= kShort) {
+        const bool wide = rows_of(16 / (int)es, H, dtype, {u, h});
         const hipError_t e = dtype == PARARNN_BF16 ? (G == 2 ? launch_walk<unsigned short, 2>(a, wide, st) : launch_walk<unsigned short, 3>(a, wide, st))
                                                    : (G == 2 ? launch_walk<float, 2>(a, wide, st) : launch_walk<float, 3>(a, wide, st));
         return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
     }
-    char *ws = static_cast<char *>(workspace);
-    a.ticket = reinterpret_cast<unsigned int *>(ws);
-    a.rec = reinterpret_cast<word_t *>(ws + 256);
-    a.tag = 0; a.spin_limit = kSpinLimit;
-    if (s.n_lt > 1 && launch_clear(ws, s.bytes, st) != hipSuccess) return PARARNN_HIP_ERROR;
-    const unsigned blocks = (unsigned)s.tiles;
-    const hipError_t e = dtype == PARARNN_BF16
-                             ? (G == 2 ? launch_forward<unsigned short, 2>(a, wide, blocks, st) : launch_forward<unsigned short, 3>(a, wide, blocks, st))
-                             : (G == 2 ? launch_forward<float, 2>(a, wide, blocks, st) : launch_forward<float, 3>(a, wide, blocks, st));
-    return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
+    if (s.n_lt > 1 && !take_workspace(workspace, s, &a, st)) {
+        workspace_forget(workspace);
+        return PARARNN_HIP_ERROR;
+    }
+    const int rc = launch_of(dtype, G, a, false, rows_of(2, H, dtype, {u, h}), st);
+    if (rc != PARARNN_OK && s.n_lt > 1) workspace_forget(workspace);
+    return rc;
 }
 
 int gated_backward(int dtype, const void *u, const float *checkpoints, const int *lengths, const void *dL_dh,
@@ -669,28 +794,24 @@ int gated_backward(int dtype, const void *u, const float *checkpoints, const int
                    size_t workspace_bytes, hipStream_t st)
 {
     Shape s;
-    if (!shape_of(dtype, B, L, H, G, &s) || !u || !checkpoints || !dL_du || !workspace || misaligned(workspace, 256))
+    if (!shape_of(dtype, B, L, H, G, &s) || !u || !checkpoints || !dL_du || (!workspace && s.n_lt > 1) || misaligned(workspace, 256))
         return PARARNN_INVALID_ARG;
     const size_t es = dtype == PARARNN_BF16 ? 2 : 4;
     if (misaligned(u, es) || misaligned(dL_dh, es) || misaligned(dL_du, es) || misaligned(checkpoints, 4) || misaligned(lengths, 4) ||
         misaligned(dL_dlast, 4) || misaligned(dL_dh0, 4))
         return PARARNN_INVALID_ARG;
     if (!size_ok(s, H)) return PARARNN_UNSUPPORTED;
-    if (workspace_bytes < s.bytes) return PARARNN_WORKSPACE_TOO_SMALL;
+    if (s.n_lt > 1 && workspace_bytes < s.bytes) return PARARNN_WORKSPACE_TOO_SMALL;
     GatedArgs a = {};
     a.u = u; a.lengths = lengths; a.ckpt = const_cast<float *>(checkpoints); a.g = dL_dh; a.dlast = dL_dlast; a.du = dL_du; a.dh0 = dL_dh0;
     a.B = B; a.L = L; a.H = H; a.n_lt = s.n_lt; a.groups = s.groups; a.chains = (int)s.chains;
-    const bool wide = wide_ok(H, dtype, {u, dL_dh, dL_du});
-    char *ws = static_cast<char *>(workspace);
-    a.ticket = reinterpret_cast<unsigned int *>(ws);
-    a.rec = reinterpret_cast<word_t *>(ws + 256);
-    a.tag = 0; a.spin_limit = kSpinLimit;
-    if (s.n_lt > 1 && launch_clear(ws, s.bytes, st) != hipSuccess) return PARARNN_HIP_ERROR;
-    const unsigned blocks = (unsigned)s.tiles;
-    const hipError_t e = dtype == PARARNN_BF16
-                             ? (G == 2 ? launch_backward<unsigned short, 2>(a, wide, blocks, st) : launch_backward<unsigned short, 3>(a, wide, blocks, st))
-                             : (G == 2 ? launch_backward<float, 2>(a, wide, blocks, st) : launch_backward<float, 3>(a, wide, blocks, st));
-    return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
+    if (s.n_lt > 1 && !take_workspace(workspace, s, &a, st)) {
+        workspace_forget(workspace);
+        return PARARNN_HIP_ERROR;
+    }
+    const int rc = launch_of(dtype, G, a, true, rows_of(2, H, dtype, {u, dL_dh, dL_du}), st);
+    if (rc != PARARNN_OK && s.n_lt > 1) workspace_forget(workspace);
+    return rc;
 }
 
 }  // namespace pararnn

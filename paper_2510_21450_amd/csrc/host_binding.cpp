@@ -170,6 +170,7 @@ public:
             ws_ = own_memory(front, like);
             kept_ = pararnn_workspace_keep(ws_.data_ptr(), 1) == PARARNN_OK;
         }
+        if (rest == 0) return;
         try {
             rest_ = own_memory(rest, like);
         } catch (...) {
@@ -472,6 +473,36 @@ GatedDims gated_dims(const Tensor &u)
     return d;
 }
 
+// The gated calls' kept workspaces: all of it is a front, and the layout is the same for both directions, types and gates.
+const Cell &gated_cell()
+{
+    static Cell &c = *[] {
+        static char name;
+        Cell *r = new Cell;
+        r->what = "pararnn_gated";
+        r->fwd_fn = reinterpret_cast<Cell::Fwd>(&name);      // never called: a name no other cell has
+        r->parts_fn = [](int dtype, int B, int L, int H, int, int, size_t *rest) {
+            *rest = 0;
+            return pararnn_gated_workspace_bytes(dtype, B, L, H, 2);
+        };
+        return r;
+    }();
+    return c;
+}
+// None (an undefined tensor) where the call uses none.
+struct GatedWorkspace {
+    GatedWorkspace(const GatedDims &d, int code, const Tensor &like, const OptTensor &given, const c10::optional<int64_t> &stream)
+    {
+        const size_t bytes = pararnn_gated_workspace_bytes(code, d.B, d.L, d.H, d.G);
+        if (has(given)) check_on(*given, "workspace", at::kByte, {given->numel()}, like);
+        if (bytes > 256 || has(given)) ws.emplace(gated_cell(), false, PARARNN_F32, Dims{d.B, d.L, d.H}, 0, bytes, like, given, stream);
+    }
+    void *data() const { return ws ? ws->data() : nullptr; }
+    size_t size() const { return ws ? ws->size() : 0; }
+    void done() { if (ws) ws->done(); }
+    c10::optional<Workspace> ws;
+};
+
 struct GatedOut { Tensor h, last, ckpt; };
 
 GatedOut gated_solve(const Tensor &u, const OptTensor &h0, const OptTensor &lengths, bool checkpoints, const OptTensor &workspace,
@@ -493,12 +524,12 @@ GatedOut gated_solve(const Tensor &u, const OptTensor &h0, const OptTensor &leng
         const int64_t rows = bytes ? (int64_t)(bytes / 4 / d.B / d.H) : 0;
         r.ckpt = at::empty({d.B, rows, d.H}, u.options().dtype(at::kFloat));
     }
-    const Tensor ws = workspace_of(pararnn_gated_workspace_bytes(code, d.B, d.L, d.H, d.G), u, workspace);
+    GatedWorkspace ws(d, code, u, workspace, stream);
     raise_if(pararnn_gated_forward(code, u.data_ptr(), static_cast<const float *>(ptr(h0)), static_cast<const int *>(ptr(lengths)), d.B,
                                    d.L, d.H, d.G, r.h.data_ptr(), static_cast<float *>(r.last.data_ptr()),
-                                   checkpoints ? static_cast<float *>(r.ckpt.data_ptr()) : nullptr, ws.data_ptr(), (size_t)ws.numel(),
-                                   on.stream()),
+                                   checkpoints ? static_cast<float *>(r.ckpt.data_ptr()) : nullptr, ws.data(), ws.size(), on.stream()),
              "pararnn_gated_forward");
+    ws.done();
     return r;
 }
 
@@ -520,12 +551,12 @@ GatedGrads gated_adjoint(const Tensor &u, const Tensor &ckpt, const OptTensor &g
     r.du = has(out) ? *out : at::empty(u.sizes(), u.options());
     check_on(r.du, "dL_du", dt, u.sizes(), u);
     if (want_dh0) r.dh0 = at::empty({d.B, d.H}, u.options().dtype(at::kFloat));
-    const Tensor ws = workspace_of(pararnn_gated_workspace_bytes(code, d.B, d.L, d.H, d.G), u, workspace);
+    GatedWorkspace ws(d, code, u, workspace, stream);
     raise_if(pararnn_gated_backward(code, u.data_ptr(), static_cast<const float *>(ckpt.data_ptr()), static_cast<const int *>(ptr(lengths)),
                                     ptr(g), static_cast<const float *>(ptr(dlast)), d.B, d.L, d.H, d.G, r.du.data_ptr(),
-                                    want_dh0 ? static_cast<float *>(r.dh0.data_ptr()) : nullptr, ws.data_ptr(), (size_t)ws.numel(),
-                                    on.stream()),
+                                    want_dh0 ? static_cast<float *>(r.dh0.data_ptr()) : nullptr, ws.data(), ws.size(), on.stream()),
              "pararnn_gated_backward");
+    ws.done();
     return r;
 }
 

@@ -607,7 +607,6 @@ size_t pararnn_gated_checkpoint_bytes(int dtype, int B, int L, int H, int G) { r
 int pararnn_gated_forward(int dtype, const void *u, const float *h0, const int *lengths, int B, int L, int H, int G, void *h,
                           float *h_last, float *checkpoints, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
-    workspace_forget(workspace);
     return gated_forward(dtype, u, h0, lengths, B, L, H, G, h, h_last, checkpoints, workspace, workspace_bytes,
                          static_cast<hipStream_t>(hip_stream));
 }
@@ -616,7 +615,6 @@ int pararnn_gated_backward(int dtype, const void *u, const float *checkpoints, c
                            const float *dL_dlast, int B, int L, int H, int G, void *dL_du, float *dL_dh0, void *workspace,
                            size_t workspace_bytes, void *hip_stream)
 {
-    workspace_forget(workspace);
     return gated_backward(dtype, u, checkpoints, lengths, dL_dh, dL_dlast, B, L, H, G, dL_du, dL_dh0, workspace, workspace_bytes,
                           static_cast<hipStream_t>(hip_stream));
 }
