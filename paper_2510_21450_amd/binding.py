@@ -417,6 +417,7 @@ _lib.pararnn_input_projection_workspace_bytes.restype = _sz
 _lib.pararnn_input_projection_workspace_bytes.argtypes = [_i] * 7
 _lib.pararnn_gated_workspace_bytes.restype = _sz
 _lib.pararnn_gated_workspace_bytes.argtypes = [_i] * 5
+_lib.pararnn_q4_exact_rows.argtypes = [_i] * 3
 
 
 def input_projection_workspace_bytes(dtype, B: int, L: int, H: int, G: int, n_heads: int = 1, backward: bool = False) -> int:
@@ -482,6 +483,12 @@ def input_projection_q4(x, Wq: ProjectionQ4, bias=None, workspace=None, stream=N
     """pararnn_input_projection_q4: `input_projection` with 4-bit weights.  x [B][L][H], bias fp32 [G][H] or None ->
     u [B][L][G][H] of x's dtype.  No gradient."""
     return _host.input_projection_q4(x, Wq, bias, workspace, _raw_stream(stream), out)
+
+
+def q4_exact_rows(H: int, G: int, n_heads: int = 1) -> int:
+    """pararnn_q4_exact_rows: rows B * L up to which `input_projection_q4` multiplies bf16 inputs with the 4-bit values themselves;
+    beyond, with the values rounded to bf16."""
+    return _lib.pararnn_q4_exact_rows(H, G, n_heads)
 
 
 def gated_layer_step(x, Wq: ProjectionQ4, h=None, bias=None, stream=None, out=None):

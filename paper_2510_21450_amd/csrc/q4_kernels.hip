@@ -73,18 +73,25 @@ struct PrepArgs {
     unsigned short *Wb_out;
     int *tickets;
     int nu, group, dh;
-    long long units;              // of `per` k units each
+    int per_row;                  // k units of a row tile, PER taken as one
 };
+
+// Row tile and k unit of a wave: the grid is (row tiles, k units / 4)
+__device__ __forceinline__ bool unit_of(const PrepArgs &a, long long *rt, int *ku)
+{
+    *rt = blockIdx.x;
+    *ku = (int)(blockIdx.y * 4 + (threadIdx.x >> 6));
+    return *ku < a.per_row;
+}
 
 // A wave takes PER k units of 16 outputs: one, or the two that share a scale.  Memory-bound: 4.5 bytes a weight.
 template <int PER> __global__ __launch_bounds__(256) void q4_quantize_kernel(const PrepArgs a)
 {
-    const long long id = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (id >= a.units) return;
+    long long rt;
+    int ku;
+    if (!unit_of(a, &rt, &ku)) return;
+    ku *= PER;
     const int lane = threadIdx.x & 63, n = lane & 15, kq = lane >> 4;
-    const int per_row = a.nu / PER;
-    const long long rt = id / per_row;
-    const int ku = (int)(id - rt * per_row) * PER;
     const float *src = a.W + (rt * 16 + n) * a.dh + ku * 64 + 8 * kq;
     float v[PER * 2][8], big[PER * 2];
 #pragma unroll
@@ -123,11 +130,10 @@ template <int PER> __global__ __launch_bounds__(256) void q4_quantize_kernel(con
 
 __global__ __launch_bounds__(256) void q4_pack_kernel(const PrepArgs a)
 {
-    const long long id = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (id >= a.units) return;
+    long long rt;
+    int ku;
+    if (!unit_of(a, &rt, &ku)) return;
     const int lane = threadIdx.x & 63, n = lane & 15, kq = lane >> 4;
-    const long long rt = id / a.nu;
-    const int ku = (int)(id - rt * a.nu);
     const signed char *src = a.codes + (rt * 16 + n) * a.dh + ku * 64 + 8 * kq;
     unsigned int w[2];
 #pragma unroll
@@ -139,7 +145,7 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const PrepArgs a)
         for (int e = 0; e < 8; ++e) q[e] = c[e] < -8 ? -8 : c[e] > 7 ? 7 : c[e];
         w[s] = pack8(q);
     }
-    a.packed_out[id * 64 + lane] = u2v{w[0], w[1]};
+    a.packed_out[(rt * a.nu + ku) * 64 + lane] = u2v{w[0], w[1]};
     const int ng = a.dh / a.group;
     if (kq == 0)
         for (int k = ku * 64; k < ku * 64 + 64; k += 32)
@@ -149,13 +155,12 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const PrepArgs a)
 // Wx fp32, or rounded to bf16 for the matrix products of many rows
 template <bool BF16> __global__ __launch_bounds__(256) void q4_dequantize_kernel(const PrepArgs a)
 {
-    if (BF16 && blockIdx.x == 0 && threadIdx.x < 8) a.tickets[threadIdx.x] = 0;      // for the product that follows
-    const long long id = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (id >= a.units) return;
-    const int lane = threadIdx.x & 63, n = lane & 15, kq = lane >> 4;
-    const long long rt = id / a.nu;
-    const int ku = (int)(id - rt * a.nu), ng = a.dh / a.group;
-    const u2v w = a.packed[id * 64 + lane];
+    if (BF16 && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 8) a.tickets[threadIdx.x] = 0;      // for the product that follows
+    long long rt;
+    int ku;
+    if (!unit_of(a, &rt, &ku)) return;
+    const int lane = threadIdx.x & 63, n = lane & 15, kq = lane >> 4, ng = a.dh / a.group;
+    const u2v w = a.packed[(rt * a.nu + ku) * 64 + lane];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         const int k = ku * 64 + 32 * s;
@@ -183,8 +188,13 @@ struct RowsQ4Args {
     const float *bias, *h;
     void *out;                    // u, or y of a step
     float *h_next;
-    int rows, H, G, dh, nu, group;
+    int rows, H, G, dh;
+    int nu, ng, tiles;            // units and groups of a head's inputs; 16-channel tiles of a gate
+    int unit_shift;               // a unit's group is unit >> this (groups of 64 and 128)
 };
+
+// Waves whose sums of `tiles` KB each are in LDS at once: 64 KB
+constexpr __host__ __device__ int sums_in_lds(int tiles) { return 64 / tiles < 8 ? 64 / tiles : 8; }
 
 // Eight inputs of a row as they lie in memory, and as operands
 template <typename T> struct Eight;
@@ -218,113 +228,180 @@ template <> struct Eight<float> {
     }
 };
 
-// A workgroup: 16 channels (STEP: of all NG gates; else of one gate's rows of the weights) x 16 MT rows; its waves share the inputs of
-// a head among them and add up in LDS.  G32: groups of 32 inputs, else of 64 and more.
-template <typename T, int MT, int NG, bool STEP, bool G32>
-__global__ __launch_bounds__(512) void q4_rows_kernel(const RowsQ4Args a)
+// A workgroup: 16 CT channels (STEP: of all NG gates; else of one gate) x 16 MT rows; its waves share the inputs of a head among
+// them and add up in LDS.  A row's inputs are read once for the NG CT tiles of weights and a weight once for the 16 MT rows.
+// Few rows are bound by the way to memory and back, so a wave asks for U units at once (its whole share of up to 4096 inputs for
+// one row), and for what it adds to the sums before the first of them comes.  G32: groups of 32 inputs, else of 64 and more.
+// More than 16 rows: two sets of units in turn, the next one's loads ahead of this one's products.
+template <typename T, int MT, bool G32> constexpr int units_in_flight()
 {
-    constexpr int U = MT * NG * (sizeof(T) / 2) <= 3 ? 4 : 2;      // units in flight
+    return sizeof(T) == 2 ? (MT == 1 ? (G32 ? 6 : 8) : MT == 2 ? 2 : 1) : MT == 1 ? 4 : 1;
+}
+template <int MT> constexpr int sets_in_flight() { return MT == 1 ? 1 : 2; }
+template <typename T, int MT, int NG, int CT, bool STEP, bool G32>
+__global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel(const RowsQ4Args a)
+{
+    constexpr int U = units_in_flight<T, MT, G32>(), SETS = sets_in_flight<MT>(), NT = NG * CT;
     constexpr int TERMS = Eight<T>::TERMS;
     extern __shared__ float s_red[];
-    const int lane = threadIdx.x & 63, n = lane & 15, kq = lane >> 4, w = threadIdx.x >> 6, W = blockDim.x >> 6;
-    const int tiles = a.H / 16;                              // row tiles of a gate
-    const int g0 = STEP ? 0 : (int)blockIdx.x / tiles, ct = (int)blockIdx.x - g0 * tiles;
+    const int lane = threadIdx.x & 63, n = lane & 15, kq = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int W = blockDim.x >> 6;
+    const int per_gate = a.tiles / CT;
+    const int g0 = STEP ? 0 : (int)blockIdx.x / per_gate, ct = ((int)blockIdx.x - g0 * per_gate) * CT;
     const int m0 = (int)blockIdx.y * 16 * MT;
-    const int head = ct * 16 / a.dh, ng = a.dh / a.group;
-    const T *x = static_cast<const T *>(a.x) + (size_t)head * a.dh + 8 * kq;
+    const int head = ct * 16 / a.dh;                         // (a multiple of 64 channels: the CT tiles are of one head)
+    // bases that all lanes share, and 32-bit offsets from them
+    const T *x = static_cast<const T *>(a.x) + (size_t)m0 * a.H + (size_t)head * a.dh;
+    auto weights = [&](int g) { return a.packed + ((size_t)(g0 + g / CT) * a.tiles + ct + g % CT) * a.nu * 64; };
+    auto scales = [&](int g) { return a.scales + ((size_t)(g0 + g / CT) * a.tiles + ct + g % CT) * a.ng * 16; };
+    unsigned int at_x[MT];
+    bool row_ok[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        row_ok[m] = m0 + 16 * m + n < a.rows;
+        at_x[m] = (unsigned int)(row_ok[m] ? 16 * m + n : 0) * a.H + 8 * kq;
+    }
 
     const u4v minus24 = {0xc1c0c1c0u, 0xc1c0c1c0u, 0xc1c0c1c0u, 0xc1c0c1c0u};
     const bf8v offset = __builtin_bit_cast(bf8v, minus24);
-    f4v total[NG][MT];
+    f4v total[NT][MT];
 #pragma unroll
-    for (int g = 0; g < NG; ++g)
+    for (int g = 0; g < NT; ++g)
 #pragma unroll
         for (int m = 0; m < MT; ++m) total[g][m] = f4v{0, 0, 0, 0};
 
-    for (int base = w; base < a.nu; base += W * U) {
-        u2v q[U][NG];
-        float sc[U][NG][2];
-        Eight<T> xr[U][MT][2];
+    // sum id = ((tile of channels, 16 rows), row & 3, lane) of this workgroup, below: a lane's channels are n of every tile
+    auto row_of = [&](int id) { return m0 + 16 * (id / 256 % MT) + 4 * kq + id / 64 % 4; };
+    auto channel_of = [&](int id) { return (ct + id / (256 * MT)) * 16 + n; };
+    float bias[NT], first_h = 0.0f;
+#pragma unroll
+    for (int g = 0; g < NT; ++g) bias[g] = a.bias ? a.bias[(size_t)(g0 + g / CT) * a.H + (ct + g % CT) * 16 + n] : 0.0f;
+    if (STEP && a.h && (int)threadIdx.x < CT * MT * 256 && row_of(threadIdx.x) < a.rows)
+        first_h = a.h[(size_t)row_of(threadIdx.x) * a.H + channel_of(threadIdx.x)];
+
+    u2v q[SETS][U][NT];
+    unsigned short sc[SETS][U][NT][2];
+    Eight<T> xr[SETS][U][MT][2];
+    const int step = W * U;
+    auto load = [&](auto set, int base) {
+        constexpr int z = decltype(set)::value;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            const int unit = base + i * W;
-            const bool live = unit < a.nu;
-            const int ku = live ? unit : base;
+            const int ku = base + i * W;
+            if (ku >= a.nu) break;
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                const size_t rt = (size_t)(g0 + g) * tiles + ct;
-                q[i][g] = a.packed[(rt * a.nu + ku) * 64 + lane];
-                const unsigned short *s = a.scales + (rt * ng) * 16 + n;
+            for (int g = 0; g < NT; ++g) {
+                q[z][i][g] = weights(g)[ku * 64 + lane];
                 if constexpr (G32) {
-                    sc[i][g][0] = bf16_to_f32(s[(2 * ku) * 16]);
-                    sc[i][g][1] = bf16_to_f32(s[(2 * ku + 1) * 16]);
+                    sc[z][i][g][0] = scales(g)[2 * ku * 16 + n];
+                    sc[z][i][g][1] = scales(g)[(2 * ku + 1) * 16 + n];
                 } else {
-                    sc[i][g][0] = bf16_to_f32(s[(ku * 64 / a.group) * 16]);
+                    sc[z][i][g][0] = scales(g)[(ku >> a.unit_shift) * 16 + n];
                 }
             }
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                const int row = m0 + 16 * m + n;
-                const bool ok = live && row < a.rows;
-                const T *p = x + (size_t)(row < a.rows ? row : a.rows - 1) * a.H + ku * 64;
+            for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    xr[i][m][s].load(p + 32 * s);
-                    if (!ok) xr[i][m][s].zero();
+                for (int s = 0; s < 2; ++s) xr[z][i][m][s].load(x + (at_x[m] + (unsigned int)(ku * 64 + 32 * s)));
+        }
+    };
+    auto multiply = [&](auto set, int base) {
+        constexpr int z = decltype(set)::value;
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            if (base + i * W >= a.nu) break;
+            constexpr int PARTS = G32 ? 2 : 1, STEPS = 2 / PARTS;         // groups of a unit, steps of 32 inputs in each
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) {
+                bf8v t[MT][STEPS][TERMS];
+                f4v start[MT];
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    start[m] = f4v{0, 0, 0, 0};
+#pragma unroll
+                    for (int s = 0; s < STEPS; ++s) {
+                        if (!row_ok[m]) xr[z][i][m][p * STEPS + s].zero();
+                        xr[z][i][m][p * STEPS + s].terms(t[m][s]);
+                        if constexpr (TERMS == 1) start[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(t[m][s][0], offset, start[m], 0, 0, 0);
+                    }
+                }
+#pragma unroll
+                for (int g = 0; g < NT; ++g) {
+                    bf8v b[STEPS];
+#pragma unroll
+                    for (int s = 0; s < STEPS; ++s) b[s] = TERMS == 1 ? operand(q[z][i][g][p * STEPS + s]) : operand_signed(q[z][i][g][p * STEPS + s]);
+                    const float scale = bf16_to_f32(sc[z][i][g][p]);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        f4v acc = start[m];
+#pragma unroll
+                        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                            for (int e = TERMS - 1; e >= 0; --e) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(t[m][s][e], b[s], acc, 0, 0, 0);
+                        // a lane's four sums are rows 4 kq .. 4 kq + 3 of channel n
+                        total[g][m] += scale * acc;
+                    }
                 }
             }
         }
-#pragma unroll
-        for (int i = 0; i < U; ++i)
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                bf8v t[2][TERMS];
-                xr[i][m][0].terms(t[0]);
-                xr[i][m][1].terms(t[1]);
-                f4v start[2] = {f4v{0, 0, 0, 0}, f4v{0, 0, 0, 0}};
-                if constexpr (TERMS == 1)
-#pragma unroll
-                    for (int s = 0; s < 2; ++s)
-                        start[G32 ? s : 0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(t[s][0], offset, start[G32 ? s : 0], 0, 0, 0);
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    f4v acc = start[0];
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        const bf8v b = TERMS == 1 ? operand(q[i][g][s]) : operand_signed(q[i][g][s]);
-                        if (G32 && s == 1) {
-                            total[g][m] += sc[i][g][0] * acc;
-                            acc = start[1];
-                        }
-#pragma unroll
-                        for (int e = TERMS - 1; e >= 0; --e) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(t[s][e], b, acc, 0, 0, 0);
-                    }
-                    // a lane's four sums are rows 4 kq .. 4 kq + 3 of channel n
-                    total[g][m] += sc[i][g][G32 ? 1 : 0] * acc;
-                }
-            }
+    };
+    constexpr std::integral_constant<int, 0> first{};
+    constexpr std::integral_constant<int, SETS - 1> second{};
+    if constexpr (SETS == 1) {
+        for (int base = w; base < a.nu; base += step) {
+            load(first, base);
+            multiply(first, base);
+        }
+    } else {
+        load(first, w);
+        load(second, w + step);
+        for (int base = w; base < a.nu; base += 2 * step) {
+            multiply(first, base);
+            load(first, base + 2 * step);
+            multiply(second, base + step);
+            load(second, base + 3 * step);
+        }
     }
+    // the waves' sums, in a fixed order; halves first while LDS does not hold those of all
+    auto put = [&](int at) {
 #pragma unroll
-    for (int g = 0; g < NG; ++g)
+        for (int g = 0; g < NT; ++g)
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+            for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s_red[((w * NG + g) * MT + m) * 256 + j * 64 + lane] = total[g][m][j];
+                for (int j = 0; j < 4; ++j) s_red[((at * NT + g) * MT + m) * 256 + j * 64 + lane] = total[g][m][j];
+    };
+    for (; W > sums_in_lds(NT * MT); W /= 2) {
+        if (w >= W / 2 && w < W) put(w - W / 2);
+        __syncthreads();
+        if (w < W / 2)
+#pragma unroll
+            for (int g = 0; g < NT; ++g)
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) total[g][m][j] += s_red[((w * NT + g) * MT + m) * 256 + j * 64 + lane];
+        __syncthreads();
+    }
+    if (w < W) put(w);
     __syncthreads();
-    for (int id = threadIdx.x; id < MT * 256; id += blockDim.x) {
-        const int m = id >> 8, j = id >> 6 & 3, l = id & 63;
-        const int row = m0 + 16 * m + 4 * (l >> 4) + j, ch = ct * 16 + (l & 15);
+    for (int id = threadIdx.x; id < CT * MT * 256; id += blockDim.x) {
+        const int row = row_of(id), ch = channel_of(id), c = id / (256 * MT);
         if (row >= a.rows) continue;
         float u[NG];
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            u[g] = a.bias ? a.bias[(size_t)(g0 + g) * a.H + ch] : 0.0f;
-            for (int p = 0; p < W; ++p) u[g] += s_red[((p * NG + g) * MT) * 256 + id];
+            float sum = bias[g * CT];
+#pragma unroll
+            for (int k = 1; k < CT; ++k) sum = c == k ? bias[g * CT + k] : sum;
+            for (int p = 0; p < W; ++p) sum += s_red[(p * NT + g * CT) * MT * 256 + id];
+            u[g] = sum;
         }
         if constexpr (STEP) {
             const size_t at = (size_t)row * a.H + ch;
+            const float h = id == (int)threadIdx.x ? first_h : a.h ? a.h[at] : 0.0f;
             const float f = fast_sigmoid(u[0]), i = fast_sigmoid(NG == 2 ? -u[0] : u[NG - 2]);
-            const float next = fmaf(f, a.h ? a.h[at] : 0.0f, i * u[NG - 1]);
+            const float next = fmaf(f, h, i * u[NG - 1]);
             a.h_next[at] = next;
             if constexpr (sizeof(T) == 4) static_cast<float *>(a.out)[at] = next;
             else static_cast<unsigned short *>(a.out)[at] = f32_to_bf16(next);
@@ -337,7 +414,18 @@ __global__ __launch_bounds__(512) void q4_rows_kernel(const RowsQ4Args a)
 }
 
 // ------------------------------------------------------------------ host
-constexpr int kExactRows = 64;
+// Rows up to which bf16 inputs take q4_rows_kernel, beyond the weights are written out in bf16 for the tiles of the projection.  The
+// former does 0.3 PFLOP/s; the latter up to 1, but a tile of 128 x 128 takes 0.026 us for each input of a head whatever there
+// is beside it.  (H x gates, dh): rows at which both take the same and what that is, from 65 to 2048 rows measured: (2048 x 2, 2048)
+// 1050, 57 us; (4096 x 3, 1024) 340, 42; (8192 x 2, 1024) 270, 44; (2048 x 3, 1024) 660, 38; (1024 x 3, 256) 1100, 17;
+// (512 x 2, 256) beyond 2048.  At 128 rows: 9 us to 56, 20 to 41, 20 to 44, 11 to 35, 5.5 to 15, 3.3 to 14.
+int exact_rows(int H, int G, int n_heads)
+{
+    const double dh = H / n_heads, rows = (0.5 + 0.026 * dh) * 0.13e9 / ((double)G * H * dh);
+    return rows < 64 ? 64 : rows > 1e6 ? 1000000 : (int)rows;
+}
+constexpr int kWorkgroups = 192;        // fewer leave too much of the device idle
+
 
 bool weights_ok(int H, int G, int n_heads) { return H >= 1 && G >= 1 && G <= 8 && n_heads >= 1 && H % n_heads == 0; }
 bool group_ok(int group) { return group == 32 || group == 64 || group == 128; }
@@ -355,27 +443,44 @@ PrepArgs prep_args(int H, int G, int n_heads, int group, int per)
     a.dh = H / n_heads;
     a.nu = a.dh / 64;
     a.group = group;
-    a.units = (long long)G * H / 16 * (a.nu / per);
+    a.per_row = a.nu / per;
     return a;
 }
-unsigned prep_blocks(const PrepArgs &a) { return (unsigned)((a.units + 3) / 4); }
+dim3 prep_grid(const PrepArgs &a, int H, int G) { return dim3((unsigned)((long long)G * H / 16), (unsigned)((a.per_row + 3) / 4)); }
+dim3 prep_block(const PrepArgs &a) { return dim3(64 * (a.per_row < 4 ? a.per_row : 4)); }
 
-template <typename T, int MT, int NG, bool STEP, bool G32> hipError_t launch_rows(const RowsQ4Args &a, hipStream_t st)
+template <typename T, int MT, int NG, int CT, bool STEP> hipError_t launch_rows(const RowsQ4Args &a, int group, hipStream_t st)
 {
     int W = a.nu < 8 ? a.nu : 8;
-    const int most = 48 / (NG * MT);                          // sums of a wave: NG MT KB of LDS
-    if (W > most) W = most;
-    const unsigned tiles = (unsigned)(a.H / 16) * (STEP ? 1 : a.G), mb = (unsigned)((a.rows + 16 * MT - 1) / (16 * MT));
-    hipLaunchKernelGGL((q4_rows_kernel<T, MT, NG, STEP, G32>), dim3(tiles, mb), dim3(64 * W), (size_t)W * NG * MT * 1024, st, a);
+    const int held = sums_in_lds(NG * CT * MT);
+    if (W > held)                                             // they are halved until they fit
+        while (W & (W - 1)) --W;
+    const dim3 grid((unsigned)(a.tiles / CT) * (STEP ? 1 : a.G), (unsigned)((a.rows + 16 * MT - 1) / (16 * MT))), block(64 * W);
+    const size_t lds = (size_t)(W > held ? std::max(W / 2, held) : W) * NG * CT * MT * 1024;
+    if constexpr (MT < 4)
+        if (group == 32) {
+            hipLaunchKernelGGL((q4_rows_kernel<T, MT, NG, CT, STEP, true>), grid, block, lds, st, a);
+            return hipGetLastError();
+        }
+    hipLaunchKernelGGL((q4_rows_kernel<T, MT, NG, CT, STEP, false>), grid, block, lds, st, a);
     return hipGetLastError();
 }
-template <typename T, int NG, bool STEP> hipError_t launch_rows_of(const RowsQ4Args &a, hipStream_t st)
+// Rows and channels of a workgroup: the more, the fewer times weights and inputs are read, as long as there are workgroups for the
+// device.
+template <typename T, int NG, bool STEP> hipError_t launch_rows_of(RowsQ4Args a, int n_heads, int group, hipStream_t st)
 {
-#define PARARNN_Q4(MT) (a.group == 32 ? launch_rows<T, MT, NG, STEP, true>(a, st) : launch_rows<T, MT, NG, STEP, false>(a, st))
-    if (a.rows <= 16) return PARARNN_Q4(1);
-    if (a.rows <= 32) return PARARNN_Q4(2);
-    return PARARNN_Q4(4);
-#undef PARARNN_Q4
+    a.dh = a.H / n_heads; a.nu = a.dh / 64; a.ng = a.dh / group; a.tiles = a.H / 16;
+    a.unit_shift = group == 128 ? 1 : 0;
+    const long long tiles = (long long)a.tiles * (STEP ? 1 : a.G);
+    auto groups = [&](int mt, int ct) { return tiles / ct * ((a.rows + 16 * mt - 1) / (16 * mt)); };
+    constexpr int C4 = STEP ? 1 : 4, C2 = STEP ? 1 : 2;
+    // (groups of 32, and three terms of fp32, leave no registers for 64 rows)
+    if constexpr (sizeof(T) == 2)
+        if (group != 32 && a.rows > 32 && groups(4, C4) >= kWorkgroups) return launch_rows<T, 4, NG, C4, STEP>(a, group, st);
+    if (a.rows > 16 && groups(2, C4) >= kWorkgroups) return launch_rows<T, 2, NG, C4, STEP>(a, group, st);
+    if (a.rows > 16 && groups(2, 1) >= kWorkgroups) return launch_rows<T, 2, NG, 1, STEP>(a, group, st);
+    if (a.rows > 1 && groups(1, C2) >= kWorkgroups) return launch_rows<T, 1, NG, C2, STEP>(a, group, st);
+    return launch_rows<T, 1, NG, 1, STEP>(a, group, st);
 }
 
 }  // namespace
@@ -400,8 +505,8 @@ int q4_quantize(const float *Wx, int H, int G, int n_heads, int group, void *pac
     if (unsupported(H, n_heads, group)) return PARARNN_UNSUPPORTED;
     PrepArgs a = prep_args(H, G, n_heads, group, group == 128 ? 2 : 1);
     a.W = Wx; a.packed_out = static_cast<u2v *>(packed); a.scales_out = static_cast<unsigned short *>(scales);
-    if (group == 128) hipLaunchKernelGGL(q4_quantize_kernel<2>, dim3(prep_blocks(a)), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(q4_quantize_kernel<1>, dim3(prep_blocks(a)), dim3(256), 0, st, a);
+    if (group == 128) hipLaunchKernelGGL(q4_quantize_kernel<2>, prep_grid(a, H, G), prep_block(a), 0, st, a);
+    else hipLaunchKernelGGL(q4_quantize_kernel<1>, prep_grid(a, H, G), prep_block(a), 0, st, a);
     return hipGetLastError() == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
 }
 
@@ -415,7 +520,7 @@ int q4_pack(const signed char *codes, const void *code_scales, int H, int G, int
     PrepArgs a = prep_args(H, G, n_heads, group, 1);
     a.codes = codes; a.code_scales = static_cast<const unsigned short *>(code_scales);
     a.packed_out = static_cast<u2v *>(packed); a.scales_out = static_cast<unsigned short *>(scales);
-    hipLaunchKernelGGL(q4_pack_kernel, dim3(prep_blocks(a)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(q4_pack_kernel, prep_grid(a, H, G), prep_block(a), 0, st, a);
     return hipGetLastError() == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
 }
 
@@ -427,19 +532,19 @@ int q4_dequantize(const void *packed, const void *scales, int H, int G, int n_he
     if (unsupported(H, n_heads, group)) return PARARNN_UNSUPPORTED;
     PrepArgs a = prep_args(H, G, n_heads, group, 1);
     a.packed = static_cast<const u2v *>(packed); a.scales = static_cast<const unsigned short *>(scales); a.W_out = Wx;
-    hipLaunchKernelGGL(q4_dequantize_kernel<false>, dim3(prep_blocks(a)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(q4_dequantize_kernel<false>, prep_grid(a, H, G), prep_block(a), 0, st, a);
     return hipGetLastError() == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
 }
 
 int q4_exact_rows(int H, int G, int n_heads)
 {
-    return weights_ok(H, G, n_heads) && !unsupported(H, n_heads, 32) ? kExactRows : -1;
+    return weights_ok(H, G, n_heads) && !unsupported(H, n_heads, 32) ? exact_rows(H, G, n_heads) : -1;
 }
 
 size_t q4_workspace_bytes(int dtype, int B, int L, int H, int G, int n_heads, int group)
 {
     if ((dtype != PARARNN_F32 && dtype != PARARNN_BF16) || B < 1 || L < 1 || (double)B * L > 1e9 || q4_scale_bytes(H, G, n_heads, group) == 0) return 0;
-    if (dtype == PARARNN_F32 || (long long)B * L <= kExactRows) return 256;
+    if (dtype == PARARNN_F32 || (long long)B * L <= exact_rows(H, G, n_heads)) return 256;
     return proj_workspace_bytes(dtype, B, L, H, G, n_heads, 0);
 }
 
@@ -456,21 +561,21 @@ int q4_project(int dtype, const void *x, const void *packed, const void *scales,
     if (need == 0) return PARARNN_INVALID_ARG;
     if (workspace_bytes < need) return PARARNN_WORKSPACE_TOO_SMALL;
     const int rows = B * L;
-    if (dtype == PARARNN_BF16 && rows > kExactRows) {
+    if (dtype == PARARNN_BF16 && rows > exact_rows(H, G, n_heads)) {
         if (misaligned(u, 16)) return PARARNN_UNSUPPORTED;
         int *tickets = nullptr;
         unsigned short *Wb = proj_weights_at(workspace, &tickets);
         PrepArgs p = prep_args(H, G, n_heads, group, 1);
         p.packed = static_cast<const u2v *>(packed); p.scales = static_cast<const unsigned short *>(scales);
         p.Wb_out = Wb; p.tickets = tickets;
-        hipLaunchKernelGGL(q4_dequantize_kernel<true>, dim3(prep_blocks(p)), dim3(256), 0, st, p);
+        hipLaunchKernelGGL(q4_dequantize_kernel<true>, prep_grid(p, H, G), prep_block(p), 0, st, p);
         if (hipGetLastError() != hipSuccess) return PARARNN_HIP_ERROR;
         return proj_product(dtype, x, Wb, bias, B, L, H, G, n_heads, u, tickets, st);
     }
     RowsQ4Args a = {};
     a.x = x; a.packed = static_cast<const u2v *>(packed); a.scales = static_cast<const unsigned short *>(scales); a.bias = bias; a.out = u;
-    a.rows = rows; a.H = H; a.G = G; a.dh = H / n_heads; a.nu = a.dh / 64; a.group = group;
-    const hipError_t e = dtype == PARARNN_BF16 ? launch_rows_of<unsigned short, 1, false>(a, st) : launch_rows_of<float, 1, false>(a, st);
+    a.rows = rows; a.H = H; a.G = G;
+    const hipError_t e = dtype == PARARNN_BF16 ? launch_rows_of<unsigned short, 1, false>(a, n_heads, group, st) : launch_rows_of<float, 1, false>(a, n_heads, group, st);
     return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
 }
 
@@ -486,10 +591,10 @@ int q4_step(int dtype, const void *x, const void *packed, const void *scales, co
     RowsQ4Args a = {};
     a.x = x; a.packed = static_cast<const u2v *>(packed); a.scales = static_cast<const unsigned short *>(scales); a.bias = bias; a.h = h;
     a.out = y; a.h_next = h_next;
-    a.rows = B; a.H = H; a.G = G; a.dh = H / n_heads; a.nu = a.dh / 64; a.group = group;
+    a.rows = B; a.H = H; a.G = G;
     const hipError_t e = dtype == PARARNN_BF16
-                             ? (G == 2 ? launch_rows_of<unsigned short, 2, true>(a, st) : launch_rows_of<unsigned short, 3, true>(a, st))
-                             : (G == 2 ? launch_rows_of<float, 2, true>(a, st) : launch_rows_of<float, 3, true>(a, st));
+                             ? (G == 2 ? launch_rows_of<unsigned short, 2, true>(a, n_heads, group, st) : launch_rows_of<unsigned short, 3, true>(a, n_heads, group, st))
+                             : (G == 2 ? launch_rows_of<float, 2, true>(a, n_heads, group, st) : launch_rows_of<float, 3, true>(a, n_heads, group, st));
     return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
 }
 

@@ -111,7 +111,8 @@ def test_q4_refusals(lib):
         for kw in (dict(dtype=2), dict(x=None), dict(x=A + 8), dict(bias=A + 2), dict(B=0)):
             assert call(**kw) == INVALID, (call, kw)
     assert project(L=0) == INVALID and project(u=A + 2) == INVALID and project(u=None) == INVALID and project(ws=A + 8) == INVALID
-    assert project(dtype=BF16, L=1000, bytes=256) == TOO_SMALL and project(dtype=BF16, L=1000, u=A + 2) == UNSUPPORTED
+    many = lib.pararnn_q4_exact_rows(128, 2, 1) + 1
+    assert project(dtype=BF16, B=1, L=many, bytes=256) == TOO_SMALL and project(dtype=BF16, B=1, L=many, u=A + 2) == UNSUPPORTED
     assert step(G=1) == INVALID and step(G=4) == INVALID and step(y=None) == INVALID and step(nxt=None) == INVALID
     assert step(h=A + 2) == INVALID and step(nxt=A + 2) == INVALID and step(B=(1 << 20) + 1) == UNSUPPORTED
 

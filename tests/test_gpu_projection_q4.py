@@ -98,9 +98,27 @@ def test_products(P, rows, G, heads, dh, group, dtype):
     u = P.input_projection_q4(x.view(B, rows // B, -1).cuda(), Wq, None if bias is None else bias.cuda())
     V = ref.values(codes, scales)
     want = ref.project(x, V, bias, heads)
-    many = dtype == torch.bfloat16 and rows > 64
+    many = dtype == torch.bfloat16 and rows > P.q4_exact_rows(heads * dh, G, heads)
     err = bound(x, V, scales, heads, rounded_weights=many) + 4 * ref.EPS * (0 if bias is None else bias.double().abs())
     ref.check(u.view(rows, G, -1), want, err, "u")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("G,heads,dh,group", [(2, 1, 1024, 128), (4, 3, 576, 32), (3, 2, 1024, 64)])
+@pytest.mark.parametrize("beyond", [0, 1, 300])
+def test_products_of_many_rows(P, beyond, G, heads, dh, group, dtype):
+    """At the border between the two ways for bf16, and behind it."""
+    rows = P.q4_exact_rows(heads * dh, G, heads) + beyond
+    assert 64 <= rows < 4000
+    gen = torch.Generator().manual_seed(rows)
+    codes, scales = ref.quantise(weights(G, heads, dh, seed=dh), group)
+    x = torch.randn(rows, heads * dh, generator=gen).to(dtype)
+    bias = torch.randn(G, heads * dh, generator=gen)
+    Wq = P.pack_projection(codes.cuda(), scales.cuda(), n_heads=heads)
+    u = P.input_projection_q4(x.view(1, rows, -1).cuda(), Wq, bias.cuda())
+    V = ref.values(codes, scales)
+    err = bound(x, V, scales, heads, rounded_weights=dtype == torch.bfloat16 and beyond > 0) + 4 * ref.EPS * bias.double().abs()
+    ref.check(u.view(rows, G, -1), ref.project(x, V, bias, heads), err, "u")
 
 
 def test_one_row_of_another_batch_is_the_same(P):
@@ -257,7 +275,7 @@ def test_refusals(P):
         (ValueError, lambda: P.input_projection_q4(x, Wq, torch.zeros(3, 256, device="cuda"))),
         (KeyError, lambda: P.input_projection_q4(x.half(), Wq)),
         (RuntimeError, lambda: P.input_projection_q4(x[:0], Wq)),
-        (RuntimeError, lambda: P.input_projection_q4(torch.zeros(1, 100, 256, device="cuda", dtype=torch.bfloat16), Wq,
+        (RuntimeError, lambda: P.input_projection_q4(torch.zeros(1, P.q4_exact_rows(256, 2, 2) + 1, 256, device="cuda", dtype=torch.bfloat16), Wq,
                                                      workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))),
         (ValueError, lambda: P.gated_layer_step(x, Wq)),
         (ValueError, lambda: P.gated_layer_step(row, Wq, row.bfloat16())),
