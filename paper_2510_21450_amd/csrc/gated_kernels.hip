@@ -29,7 +29,7 @@ constexpr int kCW = 64;                  // channels of a tile
 constexpr int kQueues = 16;              // counters that hand out tiles, kQueuePitch words apart (a line each)
 constexpr int kQueuePitch = 32;
 constexpr int kWaves = 8;                // of a tile's workgroup
-constexpr int kShort = 16;               // sequences up to this length: a thread walks them
+constexpr int kBatch = 4;                // steps that a thread which walks a sequence reads at once
 
 // ------------------------------------------------------------------ accesses
 typedef unsigned int u2v __attribute__((ext_vector_type(2)));
@@ -219,7 +219,8 @@ struct Place {
 // bounds a launch: its atomics take 12.5 ns each, 1.7 ms for 131072 tiles that move 6.4 GB.  Queue q's workgroups are
 // launched q, q + kQueues, ..., which are on one XCD, so that a line shared by two groups of channels is in its L2.
 // The last workgroup of a queue leaves the counter at zero for the next call.
-template <bool LOOK, bool REVERSE> __device__ __forceinline__ Place place_of(const GatedArgs &a, int *s_id)
+// TT: steps of a tile; kTT but where there is one along L.
+template <bool LOOK, bool REVERSE, int TT> __device__ __forceinline__ Place place_of(const GatedArgs &a, int *s_id)
 {
     Place p;
     if constexpr (LOOK) {
@@ -249,10 +250,10 @@ template <bool LOOK, bool REVERSE> __device__ __forceinline__ Place place_of(con
         len = __builtin_amdgcn_readfirstlane(a.lengths[p.b]);
         len = len < 0 ? 0 : len > a.L ? a.L : len;
     }
-    p.rows = len - p.lt * kTT;
-    p.rows = p.rows < 0 ? 0 : p.rows > kTT ? kTT : p.rows;
-    p.rows_all = a.L - p.lt * kTT;
-    p.rows_all = p.rows_all > kTT ? kTT : p.rows_all;
+    p.rows = len - p.lt * TT;
+    p.rows = p.rows < 0 ? 0 : p.rows > TT ? TT : p.rows;
+    p.rows_all = a.L - p.lt * TT;
+    p.rows_all = p.rows_all > TT ? TT : p.rows_all;
     // the same in all lanes, which the compiler does not see through the divisions: resources built from them would be used lane by lane
     p.b = __builtin_amdgcn_readfirstlane(p.b);
     p.grp = __builtin_amdgcn_readfirstlane(p.grp);
@@ -273,12 +274,13 @@ template <typename T, int G, int VEC, int W, int C, int LK>
 __global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a)
 {
     constexpr int LPR = kCW / VEC, SEG = 64 / LPR;
-    static_assert(W * SEG * C == kTT, "");
+    constexpr int TT = W * SEG * C;
+    static_assert(LK == 0 || TT == kTT, "");
     __shared__ float s_a[W][kCW], s_s[W][kCW], s_in[kCW];
     constexpr bool LOOK = LK > 0;
     __shared__ Seen<LOOK ? W : 1, LOOK ? LK : 1> s_seen;
     __shared__ int s_id;
-    const Place p = place_of<LOOK, false>(a, &s_id);
+    const Place p = place_of<LOOK, false, TT>(a, &s_id);
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sg = lane / LPR, c0 = (lane % LPR) * VEC;
     const int t0 = (w * SEG + sg) * C;
     const unsigned int es = sizeof(T), H = (unsigned int)a.H, first = (unsigned int)p.grp * kCW;
@@ -286,7 +288,7 @@ __global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a
     const unsigned int row_bytes = H * es, at_h = (active ? c0 * es : kOutside) + (unsigned int)t0 * row_bytes;
     const unsigned int at_u = at_h + (unsigned int)t0 * (G - 1) * row_bytes;
 
-    const size_t row = (size_t)p.b * a.L + (size_t)p.lt * kTT;
+    const size_t row = (size_t)p.b * a.L + (size_t)p.lt * TT;
     const buf_rsrc ru = rsrc_of(static_cast<const T *>(a.u) + row * G * H + first, extent(p.rows, G * H * es, first * es));
     Raw<T, VEC> raw[C][G];
 #pragma unroll
@@ -397,12 +399,13 @@ template <typename T, int G, int VEC, int W, int C, int LK>
 __global__ __launch_bounds__(64 * W, 4) void gated_backward_kernel(const GatedArgs a)
 {
     constexpr int LPR = kCW / VEC, SEG = 64 / LPR;
-    static_assert(W * SEG * C == kTT, "");
+    constexpr int TT = W * SEG * C;
+    static_assert(LK == 0 || TT == kTT, "");
     __shared__ float s_a[W][kCW], s_s[W][kCW], s_m[W][kCW], s_in[kCW];
     constexpr bool LOOK = LK > 0;
     __shared__ Seen<LOOK ? W : 1, LOOK ? LK : 1> s_seen;
     __shared__ int s_id;
-    const Place p = place_of<LOOK, true>(a, &s_id);
+    const Place p = place_of<LOOK, true, TT>(a, &s_id);
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sg = lane / LPR, c0 = (lane % LPR) * VEC;
     const int t0 = (w * SEG + sg) * C;
     const unsigned int es = sizeof(T), H = (unsigned int)a.H, first = (unsigned int)p.grp * kCW;
@@ -410,7 +413,7 @@ __global__ __launch_bounds__(64 * W, 4) void gated_backward_kernel(const GatedAr
     const unsigned int row_bytes = H * es, at_h = (active ? c0 * es : kOutside) + (unsigned int)t0 * row_bytes;
     const unsigned int at_u = at_h + (unsigned int)t0 * (G - 1) * row_bytes;
 
-    const size_t row = (size_t)p.b * a.L + (size_t)p.lt * kTT;
+    const size_t row = (size_t)p.b * a.L + (size_t)p.lt * TT;
     const buf_rsrc ru = rsrc_of(static_cast<const T *>(a.u) + row * G * H + first, extent(p.rows, G * H * es, first * es));
     const buf_rsrc rg = rsrc_of(static_cast<const T *>(a.g) + row * H + first, extent(a.g ? p.rows : 0, H * es, first * es));
     Raw<T, VEC> raw[C][G], rawg[C];
@@ -574,7 +577,7 @@ __global__ __launch_bounds__(64 * W, 4) void gated_backward_kernel(const GatedAr
     }
 }
 
-// A few steps: a thread walks them for VEC channels.  One launch, no workspace; bound by latency.
+// A few steps: a thread walks them for VEC channels, kBatch steps read at once.  One launch, no workspace; bound by latency.
 template <typename T, int G, int VEC> __global__ __launch_bounds__(256) void gated_walk_kernel(const GatedArgs a)
 {
     const int per_row = a.H / VEC;
@@ -588,48 +591,38 @@ template <typename T, int G, int VEC> __global__ __launch_bounds__(256) void gat
     }
     const T *u = static_cast<const T *>(a.u) + (size_t)b * a.L * G * a.H + c0;
     T *h = static_cast<T *>(a.h) + (size_t)b * a.L * a.H + c0;
-    auto read = [](const T *p) {
-        Raw<T, VEC> x;
-        if constexpr (sizeof(x) == 16) *reinterpret_cast<u4v *>(x.w) = *reinterpret_cast<const u4v *>(p);
-        else if constexpr (sizeof(T) == 4) x.w[0] = *reinterpret_cast<const unsigned int *>(p);
-        else x.w[0] = *reinterpret_cast<const unsigned short *>(p);
-        return x;
-    };
+    using E = typename RawVec<T, VEC>::type;
     float x[VEC];
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
         x[k] = a.h0 ? a.h0[(size_t)b * a.H + c0 + k] : 0.0f;
         if (a.ckpt) a.ckpt[(size_t)b * a.H + c0 + k] = x[k];
     }
-    for (int t = 0; t < a.L; ++t) {
-        float o[VEC];
-        if (t < len) {
-            Raw<T, VEC> r[G];
+    for (int t = 0; t < a.L; t += kBatch) {
+        E r[kBatch][G];
 #pragma unroll
-            for (int g = 0; g < G; ++g) r[g] = read(u + ((size_t)t * G + g) * a.H);
+        for (int j = 0; j < kBatch; ++j)
+            if (t + j < len)
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                float f, i;
-                sigmoid2(r[0].at(k), &f, &i);
-                if constexpr (G == 3) i = fast_sigmoid(r[1].at(k));
-                x[k] = fmaf(f, x[k], i * r[G - 1].at(k));
-                o[k] = x[k];
+                for (int g = 0; g < G; ++g) r[j][g] = *reinterpret_cast<const E *>(u + ((size_t)(t + j) * G + g) * a.H);
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            if (t + j >= a.L) break;
+            float o[VEC] = {};
+            if (t + j < len) {
+                float in[G][VEC];
+#pragma unroll
+                for (int g = 0; g < G; ++g) raw_to_float<T, VEC>(r[j][g], in[g]);
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) {
+                    float f, i;
+                    sigmoid2(in[0][k], &f, &i);
+                    if constexpr (G == 3) i = fast_sigmoid(in[1][k]);
+                    x[k] = fmaf(f, x[k], i * in[G - 1][k]);
+                    o[k] = x[k];
+                }
             }
-        } else {
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) o[k] = 0.0f;
-        }
-        T *at = h + (size_t)t * a.H;
-        if constexpr (sizeof(T) == 4) {
-            if constexpr (VEC == 4) *reinterpret_cast<float4 *>(at) = make_float4(o[0], o[1], o[2], o[3]);
-            else *at = o[0];
-        } else if constexpr (VEC == 8) {
-            unsigned int w[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = f32_to_bf16(o[2 * k]) | (unsigned int)f32_to_bf16(o[2 * k + 1]) << 16;
-            *reinterpret_cast<uint4 *>(at) = make_uint4(w[0], w[1], w[2], w[3]);
-        } else {
-            *at = f32_to_bf16(o[0]);
+            store_vec<VEC>(h + (size_t)(t + j) * a.H, o);
         }
     }
     if (a.last)
@@ -685,10 +678,10 @@ hipError_t launch_clear(void *ws, size_t bytes, hipStream_t st)
     return hipGetLastError();
 }
 
-// LK: 0 for a single tile along L
-template <typename T, int G, int VEC, int LK> void launch_tiles(const GatedArgs &a, bool backward, hipStream_t st)
+// LK: 0 for a single tile along L, of TT steps
+template <typename T, int G, int VEC, int LK, int TT = kTT> void launch_tiles(const GatedArgs &a, bool backward, hipStream_t st)
 {
-    constexpr int C = kTT / (kWaves * (64 * VEC / kCW));
+    constexpr int C = TT / (kWaves * (64 * VEC / kCW));
     const dim3 grid((unsigned)a.chains * a.n_lt), block(64 * kWaves);
     if (backward) hipLaunchKernelGGL((gated_backward_kernel<T, G, VEC, kWaves, C, LK>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((gated_forward_kernel<T, G, VEC, kWaves, C, LK>), grid, block, 0, st, a);
@@ -698,7 +691,9 @@ template <typename T, int G> hipError_t launch_tiles_of(const GatedArgs &a, bool
     const int look = a.n_lt == 1 ? 0 : wide_look(a) ? 4 : 1;
 #define PARARNN_GATED(VEC)                                                    \
     do {                                                                      \
-        if (look == 0) launch_tiles<T, G, VEC, 0>(a, backward, st);           \
+        if (look == 0 && a.L <= 32) launch_tiles<T, G, VEC, 0, 32>(a, backward, st); \
+        else if (look == 0 && a.L <= 64) launch_tiles<T, G, VEC, 0, 64>(a, backward, st); \
+        else if (look == 0) launch_tiles<T, G, VEC, 0>(a, backward, st);      \
         else if (look == 1) launch_tiles<T, G, VEC, 1>(a, backward, st);      \
         else launch_tiles<T, G, VEC, 4>(a, backward, st);                     \
     } while (0)
@@ -716,12 +711,11 @@ int launch_of(int dtype, int G, const GatedArgs &a, bool backward, bool pairs, h
     return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
 }
 
-template <typename T, int G> hipError_t launch_walk(const GatedArgs &a, bool wide, hipStream_t st)
+template <typename T, int G> hipError_t launch_walk(const GatedArgs &a, bool pairs, hipStream_t st)
 {
-    constexpr int V = 16 / sizeof(T);
-    const long long n = (long long)a.B * (a.H / (wide ? V : 1));
+    const long long n = (long long)a.B * (a.H / (pairs ? 2 : 1));
     const unsigned blocks = (unsigned)((n + 255) / 256);
-    if (wide) hipLaunchKernelGGL((gated_walk_kernel<T, G, V>), dim3(blocks), dim3(256), 0, st, a);
+    if (pairs) hipLaunchKernelGGL((gated_walk_kernel<T, G, 2>), dim3(blocks), dim3(256), 0, st, a);
     else hipLaunchKernelGGL((gated_walk_kernel<T, G, 1>), dim3(blocks), dim3(256), 0, st, a);
     return hipGetLastError();
 }
@@ -743,6 +737,11 @@ bool take_workspace(void *workspace, const Shape &s, GatedArgs *a, hipStream_t s
     a->tag = workspace_epoch(workspace, sig ? sig : 1, st, &fill);
     return !fill || launch_clear(ws, s.bytes, st) == hipSuccess;
 }
+
+// A walk takes 2 us and 0.1 to 0.2 for a step; a tile of 32 steps 2.5 to 2.8 us, from 30000 channels on more: 65536 (B x H) 4.5 to 5.6, 262144
+// 15 to 20, whatever there is of its steps.  Channels, steps at which both took the same (bf16 two gates / fp32 three): 512 6 / 4, 8192
+// 6 / 5, 65536 16 / 14, 262144 beyond 48 (a tile of 64 there) / 36.
+bool walked(int B, int L, int H) { return L <= 48 && L <= 5 + (long long)B * H / 6500; }
 
 bool misaligned(const void *p, size_t n) { return (uintptr_t)p % n != 0; }
 
@@ -774,10 +773,10 @@ int gated_forward(int dtype, const void *u, const float *h0, const int *lengths,
     GatedArgs a = {};
     a.u = u; a.h0 = h0; a.lengths = lengths; a.h = h; a.last = h_last; a.ckpt = checkpoints;
     a.B = B; a.L = L; a.H = H; a.n_lt = s.n_lt; a.groups = s.groups; a.chains = (int)s.chains;
-    if (L <= kShort) {
-        const bool wide = rows_of(16 / (int)es, H, dtype, {u, h});
-        const hipError_t e = dtype == PARARNN_BF16 ? (G == 2 ? launch_walk<unsigned short, 2>(a, wide, st) : launch_walk<unsigned short, 3>(a, wide, st))
-                                                   : (G == 2 ? launch_walk<float, 2>(a, wide, st) : launch_walk<float, 3>(a, wide, st));
+    if (walked(B, L, H)) {
+        const bool pairs = rows_of(2, H, dtype, {u, h});
+        const hipError_t e = dtype == PARARNN_BF16 ? (G == 2 ? launch_walk<unsigned short, 2>(a, pairs, st) : launch_walk<unsigned short, 3>(a, pairs, st))
+                                                   : (G == 2 ? launch_walk<float, 2>(a, pairs, st) : launch_walk<float, 3>(a, pairs, st));
         return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
     }
     if (s.n_lt > 1 && !take_workspace(workspace, s, &a, st)) {

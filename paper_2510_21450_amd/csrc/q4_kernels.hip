@@ -74,13 +74,16 @@ struct PrepArgs {
     int *tickets;
     int nu, group, dh;
     int per_row;                  // k units of a row tile, PER taken as one
+    unsigned int blocks;          // workgroups that share a row tile, four units each
 };
 
-// Row tile and k unit of a wave: the grid is (row tiles, k units / 4)
+// Row tile and k unit of a wave.  Neighbouring workgroups take neighbouring units of the same rows (the other order: 55 -> 68 us for 2 x 4096
+// x 4096 weights to 4 bits and back).
 __device__ __forceinline__ bool unit_of(const PrepArgs &a, long long *rt, int *ku)
 {
-    *rt = blockIdx.x;
-    *ku = (int)(blockIdx.y * 4 + (threadIdx.x >> 6));
+    const unsigned int r = blockIdx.x / a.blocks;
+    *rt = r;
+    *ku = (int)((blockIdx.x - r * a.blocks) * 4 + (threadIdx.x >> 6));
     return *ku < a.per_row;
 }
 
@@ -155,7 +158,7 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const PrepArgs a)
 // Wx fp32, or rounded to bf16 for the matrix products of many rows
 template <bool BF16> __global__ __launch_bounds__(256) void q4_dequantize_kernel(const PrepArgs a)
 {
-    if (BF16 && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 8) a.tickets[threadIdx.x] = 0;      // for the product that follows
+    if (BF16 && blockIdx.x == 0 && threadIdx.x < 8) a.tickets[threadIdx.x] = 0;      // for the product that follows
     long long rt;
     int ku;
     if (!unit_of(a, &rt, &ku)) return;
@@ -429,11 +432,11 @@ constexpr int kWorkgroups = 192;        // fewer leave too much of the device id
 
 bool weights_ok(int H, int G, int n_heads) { return H >= 1 && G >= 1 && G <= 8 && n_heads >= 1 && H % n_heads == 0; }
 bool group_ok(int group) { return group == 32 || group == 64 || group == 128; }
-// what the kernels have no form for
+// what the kernels have no form for (2^38 weights a gate: workgroups are numbered in 32 bits)
 bool unsupported(int H, int n_heads, int group)
 {
     const int dh = H / n_heads;
-    return H > (1 << 20) || dh % 64 || dh % group;
+    return H > (1 << 20) || dh % 64 || dh % group || (double)H * dh > 2.7e11;
 }
 bool misaligned(const void *p, size_t n) { return (uintptr_t)p % n != 0; }
 
@@ -444,9 +447,10 @@ PrepArgs prep_args(int H, int G, int n_heads, int group, int per)
     a.nu = a.dh / 64;
     a.group = group;
     a.per_row = a.nu / per;
+    a.blocks = (unsigned)(a.per_row + 3) / 4;
     return a;
 }
-dim3 prep_grid(const PrepArgs &a, int H, int G) { return dim3((unsigned)((long long)G * H / 16), (unsigned)((a.per_row + 3) / 4)); }
+dim3 prep_grid(const PrepArgs &a, int H, int G) { return dim3((unsigned)((long long)G * H / 16) * a.blocks); }
 dim3 prep_block(const PrepArgs &a) { return dim3(64 * (a.per_row < 4 ? a.per_row : 4)); }
 
 template <typename T, int MT, int NG, int CT, bool STEP> hipError_t launch_rows(const RowsQ4Args &a, int group, hipStream_t st)
