@@ -203,26 +203,26 @@ constexpr __host__ __device__ int sums_in_lds(int tiles) { return 64 / tiles < 8
 template <typename T> struct Eight;
 template <> struct Eight<unsigned short> {
     static constexpr int TERMS = 1;
-    u4v v;
-    __device__ __forceinline__ void load(const unsigned short *p) { v = *reinterpret_cast<const u4v *>(p); }
-    __device__ __forceinline__ void zero() { v = u4v{0, 0, 0, 0}; }
-    __device__ __forceinline__ void terms(bf8v (&t)[1]) const { t[0] = __builtin_bit_cast(bf8v, v); }
+    static constexpr int CHUNKS = 1;       // of 16 bytes
+    u4v c[1];
+    __device__ __forceinline__ void load(const unsigned short *p) { c[0] = *reinterpret_cast<const u4v *>(p); }
+    __device__ __forceinline__ void terms(bf8v (&t)[1]) const { t[0] = __builtin_bit_cast(bf8v, c[0]); }
 };
 template <> struct Eight<float> {
     static constexpr int TERMS = 3;
-    f4v lo, hi;
+    static constexpr int CHUNKS = 2;
+    u4v c[2];
     __device__ __forceinline__ void load(const float *p)
     {
-        lo = *reinterpret_cast<const f4v *>(p);
-        hi = *reinterpret_cast<const f4v *>(p + 4);
+        c[0] = *reinterpret_cast<const u4v *>(p);
+        c[1] = *reinterpret_cast<const u4v *>(p + 4);
     }
-    __device__ __forceinline__ void zero() { lo = hi = f4v{0, 0, 0, 0}; }
     // x = t0 + t1 + t2: what a term leaves is exact in fp32, and eight bits of mantissa three times are all 24
     __device__ __forceinline__ void terms(bf8v (&t)[3]) const
     {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float x = e < 4 ? lo[e & 3] : hi[e & 3];
+            const float x = __uint_as_float(c[e >> 2][e & 3]);
             t[0][e] = (__bf16)x;
             const float r = x - (float)t[0][e];
             t[1][e] = (__bf16)r;
@@ -233,37 +233,26 @@ template <> struct Eight<float> {
 
 // A workgroup: 16 CT channels (STEP: of all NG gates; else of one gate) x 16 MT rows; its waves share the inputs of a head among
 // them and add up in LDS.  A row's inputs are read once for the NG CT tiles of weights and a weight once for the 16 MT rows.
-// Few rows are bound by the way to memory and back, so a wave asks for U units at once (its whole share of up to 4096 inputs for
+// Few rows are bound by the way to memory and back, so a wave asks for its units at once (its whole share of up to 4096 inputs for
 // one row), and for what it adds to the sums before the first of them comes.  G32: groups of 32 inputs, else of 64 and more.
-// More than 16 rows: two sets of units in turn, the next one's loads ahead of this one's products.
-template <typename T, int MT, bool G32> constexpr int units_in_flight()
-{
-    return sizeof(T) == 2 ? (MT == 1 ? (G32 ? 6 : 8) : MT == 2 ? 2 : 1) : MT == 1 ? 4 : 1;
-}
-template <int MT> constexpr int sets_in_flight() { return MT == 1 ? 1 : 2; }
 template <typename T, int MT, int NG, int CT, bool STEP, bool G32>
 __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel(const RowsQ4Args a)
 {
-    constexpr int U = units_in_flight<T, MT, G32>(), SETS = sets_in_flight<MT>(), NT = NG * CT;
+    constexpr int NT = NG * CT;
     constexpr int TERMS = Eight<T>::TERMS;
-    extern __shared__ float s_red[];
+    extern __shared__ __align__(16) float s_red[];
     const int lane = threadIdx.x & 63, n = lane & 15, kq = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int W = blockDim.x >> 6;
     const int per_gate = a.tiles / CT;
     const int g0 = STEP ? 0 : (int)blockIdx.x / per_gate, ct = ((int)blockIdx.x - g0 * per_gate) * CT;
     const int m0 = (int)blockIdx.y * 16 * MT;
     const int head = ct * 16 / a.dh;                         // (a multiple of 64 channels: the CT tiles are of one head)
-    // bases that all lanes share, and 32-bit offsets from them
+    // bases that all lanes share, and 32-bit offsets from them.  Rows behind the last are read as the block's first: a row of x
+    // reaches that row's sums alone, and those are not written.
     const T *x = static_cast<const T *>(a.x) + (size_t)m0 * a.H + (size_t)head * a.dh;
     auto weights = [&](int g) { return a.packed + ((size_t)(g0 + g / CT) * a.tiles + ct + g % CT) * a.nu * 64; };
     auto scales = [&](int g) { return a.scales + ((size_t)(g0 + g / CT) * a.tiles + ct + g % CT) * a.ng * 16; };
-    unsigned int at_x[MT];
-    bool row_ok[MT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        row_ok[m] = m0 + 16 * m + n < a.rows;
-        at_x[m] = (unsigned int)(row_ok[m] ? 16 * m + n : 0) * a.H + 8 * kq;
-    }
+    auto row_at = [&](int r) { return (unsigned int)(m0 + r < a.rows ? r : 0) * a.H; };
 
     const u4v minus24 = {0xc1c0c1c0u, 0xc1c0c1c0u, 0xc1c0c1c0u, 0xc1c0c1c0u};
     const bf8v offset = __builtin_bit_cast(bf8v, minus24);
@@ -282,88 +271,119 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
     if (STEP && a.h && (int)threadIdx.x < CT * MT * 256 && row_of(threadIdx.x) < a.rows)
         first_h = a.h[(size_t)row_of(threadIdx.x) * a.H + channel_of(threadIdx.x)];
 
-    u2v q[SETS][U][NT];
-    unsigned short sc[SETS][U][NT][2];
-    Eight<T> xr[SETS][U][MT][2];
-    const int step = W * U;
-    auto load = [&](auto set, int base) {
-        constexpr int z = decltype(set)::value;
+    // one unit's products; x(m, s): the eight inputs of 16 rows m at step s that this lane multiplies
+    auto multiply = [&](const u2v (&q)[NT], const unsigned short (&sc)[NT][2], auto &&x_at) {
+        constexpr int PARTS = G32 ? 2 : 1, STEPS = 2 / PARTS;             // groups of a unit, steps of 32 inputs in each
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int ku = base + i * W;
-            if (ku >= a.nu) break;
+        for (int p = 0; p < PARTS; ++p) {
+            bf8v t[MT][STEPS][TERMS];
+            f4v start[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                start[m] = f4v{0, 0, 0, 0};
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) {
+                    x_at(m, p * STEPS + s).terms(t[m][s]);
+                    if constexpr (TERMS == 1) start[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(t[m][s][0], offset, start[m], 0, 0, 0);
+                }
+            }
 #pragma unroll
             for (int g = 0; g < NT; ++g) {
-                q[z][i][g] = weights(g)[ku * 64 + lane];
-                if constexpr (G32) {
-                    sc[z][i][g][0] = scales(g)[2 * ku * 16 + n];
-                    sc[z][i][g][1] = scales(g)[(2 * ku + 1) * 16 + n];
-                } else {
-                    sc[z][i][g][0] = scales(g)[(ku >> a.unit_shift) * 16 + n];
-                }
-            }
+                bf8v b[STEPS];
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int s = 0; s < 2; ++s) xr[z][i][m][s].load(x + (at_x[m] + (unsigned int)(ku * 64 + 32 * s)));
-        }
-    };
-    auto multiply = [&](auto set, int base) {
-        constexpr int z = decltype(set)::value;
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-            if (base + i * W >= a.nu) break;
-            constexpr int PARTS = G32 ? 2 : 1, STEPS = 2 / PARTS;         // groups of a unit, steps of 32 inputs in each
-#pragma unroll
-            for (int p = 0; p < PARTS; ++p) {
-                bf8v t[MT][STEPS][TERMS];
-                f4v start[MT];
+                for (int s = 0; s < STEPS; ++s) b[s] = TERMS == 1 ? operand(q[g][p * STEPS + s]) : operand_signed(q[g][p * STEPS + s]);
+                const float scale = bf16_to_f32(sc[g][p]);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                    start[m] = f4v{0, 0, 0, 0};
+                    f4v acc = start[m];
 #pragma unroll
-                    for (int s = 0; s < STEPS; ++s) {
-                        if (!row_ok[m]) xr[z][i][m][p * STEPS + s].zero();
-                        xr[z][i][m][p * STEPS + s].terms(t[m][s]);
-                        if constexpr (TERMS == 1) start[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(t[m][s][0], offset, start[m], 0, 0, 0);
-                    }
-                }
+                    for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-                for (int g = 0; g < NT; ++g) {
-                    bf8v b[STEPS];
-#pragma unroll
-                    for (int s = 0; s < STEPS; ++s) b[s] = TERMS == 1 ? operand(q[z][i][g][p * STEPS + s]) : operand_signed(q[z][i][g][p * STEPS + s]);
-                    const float scale = bf16_to_f32(sc[z][i][g][p]);
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        f4v acc = start[m];
-#pragma unroll
-                        for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-                            for (int e = TERMS - 1; e >= 0; --e) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(t[m][s][e], b[s], acc, 0, 0, 0);
-                        // a lane's four sums are rows 4 kq .. 4 kq + 3 of channel n
-                        total[g][m] += scale * acc;
-                    }
+                        for (int e = TERMS - 1; e >= 0; --e) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(t[m][s][e], b[s], acc, 0, 0, 0);
+                    // a lane's four sums are rows 4 kq .. 4 kq + 3 of channel n
+                    total[g][m] += scale * acc;
                 }
             }
         }
     };
-    constexpr std::integral_constant<int, 0> first{};
-    constexpr std::integral_constant<int, SETS - 1> second{};
-    if constexpr (SETS == 1) {
-        for (int base = w; base < a.nu; base += step) {
-            load(first, base);
-            multiply(first, base);
+    auto load_weights = [&](int ku, u2v (&q)[NT], unsigned short (&sc)[NT][2]) {
+#pragma unroll
+        for (int g = 0; g < NT; ++g) {
+            q[g] = weights(g)[ku * 64 + lane];
+            if constexpr (G32) {
+                sc[g][0] = scales(g)[2 * ku * 16 + n];
+                sc[g][1] = scales(g)[(2 * ku + 1) * 16 + n];
+            } else {
+                sc[g][0] = scales(g)[(ku >> a.unit_shift) * 16 + n];
+            }
+        }
+    };
+    if constexpr (MT == 1) {
+        constexpr int U = sizeof(T) == 2 ? (G32 ? 6 : 8) : 4;             // units asked for at once
+        const unsigned int at = row_at(n) + 8 * kq;
+        for (int base = w; base < a.nu; base += W * U) {
+            u2v q[U][NT];
+            unsigned short sc[U][NT][2];
+            Eight<T> xr[U][2];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int ku = base + i * W;
+                if (ku >= a.nu) break;
+                load_weights(ku, q[i], sc[i]);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) xr[i][s].load(x + (at + (unsigned int)(ku * 64 + 32 * s)));
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                if (base + i * W >= a.nu) break;
+                multiply(q[i], sc[i], [&](int, int s) -> const Eight<T> & { return xr[i][s]; });
+            }
         }
     } else {
-        load(first, w);
-        load(second, w + step);
-        for (int base = w; base < a.nu; base += 2 * step) {
-            multiply(first, base);
-            load(first, base + 2 * step);
-            multiply(second, base + step);
-            load(second, base + 3 * step);
+        // Rows are read along themselves and turned in LDS, where a wave has a place for its unit of x to itself: lanes that each read a row of
+        // their own (the operand's order) touch 64 lines in one load.  A row's 16-byte chunks are turned round by its number, so that the
+        // eight lanes of a read's quarter find them in eight different places.  The next unit is on its way from memory while this one is multiplied.
+        constexpr int CH = 4 * sizeof(T), LOADS = MT * 16 * CH / 64;      // chunks of a row's 64 inputs; chunks a lane brings
+        u4v *const mine = reinterpret_cast<u4v *>(s_red) + w * (MT * 16 * CH);
+        unsigned int from[LOADS], to[LOADS];
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const int id = j * 64 + lane, r = id / CH, c = id % CH;
+            from[j] = row_at(r) + c * (16 / sizeof(T));
+            to[j] = r * CH + (c ^ (r & (CH - 1)));
         }
+        u4v raw[LOADS];
+        u2v q[NT], q_next[NT];
+        unsigned short sc[NT][2], sc_next[NT][2];
+        auto load = [&](int ku) {
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) raw[j] = *reinterpret_cast<const u4v *>(x + (from[j] + (unsigned int)ku * 64));
+            load_weights(ku, q_next, sc_next);
+        };
+        if (w < a.nu) load(w);
+        for (int ku = w; ku < a.nu; ku += W) {
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) mine[to[j]] = raw[j];
+#pragma unroll
+            for (int g = 0; g < NT; ++g) {
+                q[g] = q_next[g];
+                sc[g][0] = sc_next[g][0];
+                sc[g][1] = sc_next[g][1];
+            }
+            __builtin_amdgcn_wave_barrier();
+            if (ku + W < a.nu) load(ku + W);
+            multiply(q, sc, [&](int m, int s) {
+                Eight<T> e;
+#pragma unroll
+                for (int k = 0; k < Eight<T>::CHUNKS; ++k) {
+                    const int c = (4 * s + kq) * Eight<T>::CHUNKS + k;
+                    e.c[k] = mine[(16 * m + n) * CH + (c ^ (n & (CH - 1)))];
+                }
+                return e;
+            });
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();                                                  // the places are where the sums go
     }
     // the waves' sums, in a fixed order; halves first while LDS does not hold those of all
     auto put = [&](int at) {
@@ -460,7 +480,8 @@ template <typename T, int MT, int NG, int CT, bool STEP> hipError_t launch_rows(
     if (W > held)                                             // they are halved until they fit
         while (W & (W - 1)) --W;
     const dim3 grid((unsigned)(a.tiles / CT) * (STEP ? 1 : a.G), (unsigned)((a.rows + 16 * MT - 1) / (16 * MT))), block(64 * W);
-    const size_t lds = (size_t)(W > held ? std::max(W / 2, held) : W) * NG * CT * MT * 1024;
+    const size_t sums = (size_t)(W > held ? std::max(W / 2, held) : W) * NG * CT * MT * 1024;
+    const size_t lds = MT == 1 ? sums : std::max(sums, (size_t)W * MT * 16 * 64 * sizeof(T));
     if constexpr (MT < 4)
         if (group == 32) {
             hipLaunchKernelGGL((q4_rows_kernel<T, MT, NG, CT, STEP, true>), grid, block, lds, st, a);
