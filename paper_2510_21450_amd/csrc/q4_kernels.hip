@@ -491,20 +491,22 @@ template <typename T, int MT, int NG, int CT, bool STEP> hipError_t launch_rows(
     return hipGetLastError();
 }
 // Rows and channels of a workgroup: the more, the fewer times weights and inputs are read, as long as there are workgroups for the
-// device.
+// device.  bf16, up to 16 rows, 16 x 16 against 32 x 64 (a step: 32 x 16 of each gate): 3 x 4096 x 4096 weights 15.2 to 19.9 us -> 11.7;
+// a step with 2 x 8192 x 1024 6.1 to 7.0 -> 5.5, with 2 x 4096 x 4096 8.6 to 9.8 -> 8.5 to 8.7; fewer workgroups lose, 3 x 2048 x 1024
+// 3.5 -> 5.3.  fp32, whose terms cost more than the weights, only gains beyond 16 rows.
 template <typename T, int NG, bool STEP> hipError_t launch_rows_of(RowsQ4Args a, int n_heads, int group, hipStream_t st)
 {
     a.dh = a.H / n_heads; a.nu = a.dh / 64; a.ng = a.dh / group; a.tiles = a.H / 16;
     a.unit_shift = group == 128 ? 1 : 0;
     const long long tiles = (long long)a.tiles * (STEP ? 1 : a.G);
-    auto groups = [&](int mt, int ct) { return tiles / ct * ((a.rows + 16 * mt - 1) / (16 * mt)); };
-    constexpr int C4 = STEP ? 1 : 4, C2 = STEP ? 1 : 2;
+    auto enough = [&](int mt, int ct) { return tiles / ct * ((a.rows + 16 * mt - 1) / (16 * mt)) >= kWorkgroups; };
+    constexpr int C4 = STEP ? 1 : 4;
+    constexpr bool bf16 = sizeof(T) == 2;
     // (groups of 32, and three terms of fp32, leave no registers for 64 rows)
-    if constexpr (sizeof(T) == 2)
-        if (group != 32 && a.rows > 32 && groups(4, C4) >= kWorkgroups) return launch_rows<T, 4, NG, C4, STEP>(a, group, st);
-    if (a.rows > 16 && groups(2, C4) >= kWorkgroups) return launch_rows<T, 2, NG, C4, STEP>(a, group, st);
-    if (a.rows > 16 && groups(2, 1) >= kWorkgroups) return launch_rows<T, 2, NG, 1, STEP>(a, group, st);
-    if (a.rows > 1 && groups(1, C2) >= kWorkgroups) return launch_rows<T, 1, NG, C2, STEP>(a, group, st);
+    if constexpr (bf16)
+        if (group != 32 && a.rows > 32 && enough(4, C4)) return launch_rows<T, 4, NG, C4, STEP>(a, group, st);
+    if ((bf16 || a.rows > 16) && enough(2, C4)) return launch_rows<T, 2, NG, C4, STEP>(a, group, st);
+    if (a.rows > 16 && enough(2, 1)) return launch_rows<T, 2, NG, 1, STEP>(a, group, st);
     return launch_rows<T, 1, NG, 1, STEP>(a, group, st);
 }
 
