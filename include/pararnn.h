@@ -465,9 +465,11 @@ int pararnn_input_projection_backward(int dtype, const void *x, const float *Wx,
  * Gradients, with lam_l the gradient of h_l: lam_l = g_l + f_{l+1} lam_{l+1} (+ dL_dlast behind the
  * last step), dv = lam i, du_i = lam v i (1 - i), du_f = lam h_{l-1} f (1 - f), for G = 2
  * du_f = lam (h_{l-1} - v) f (1 - f), dL_dh0 = f_1 lam_1.
- * Arithmetic in fp32; h and dL_du are rounded once.  Results are bit-reproducible.  Tensors need the alignment of their elements; 16 bytes and H a multiple of 16 bytes
- * of elements take wide accesses.  H <= 1 048 576 (else UNSUPPORTED).  Any number of calls may run
- * at once on workspaces of their own; a call captured into a graph may be replayed.
+ * Arithmetic in fp32; h and dL_du are rounded once.  Results are bit-reproducible.  Tensors need
+ * the alignment of their elements; an even H and the alignment of two are faster.  H <= 1 048 576,
+ * B * H < 2^32 and less than 2^23 tiles of 64 channels x 128 timesteps (else UNSUPPORTED).  A wait that
+ * runs out (see pararnn_set_spin_limit; it takes a broken promise for the workspace) gives NaN from there on.  Any number
+ * of calls may run at once on workspaces of their own; a call captured into a graph may be replayed.
  */
 size_t pararnn_gated_workspace_bytes(int dtype, int B, int L, int H, int G);
 size_t pararnn_gated_checkpoint_bytes(int dtype, int B, int L, int H, int G);
@@ -482,7 +484,7 @@ int pararnn_gated_backward(int dtype, const void *u, const float *checkpoints, c
  * The input projection with 4-bit weights, for serving: Wx[g][h][j] = code * scale with codes
  * -8 .. 7 and one bf16 scale for every `group` (32, 64 or 128) consecutive inputs j of an output.
  * G, H, n_heads, dh = H / n_heads and x, u, bias as for pararnn_input_projection; dh must be a
- * multiple of 64 and of group, G <= 8, H <= 1 048 576 (else UNSUPPORTED).
+ * multiple of 64 and of group, H <= 1 048 576 and G * H * dh <= 6e10 (else UNSUPPORTED), G <= 8.
  *   packed          pararnn_q4_packed_bytes() = G * H * dh / 2 bytes, device, 16-byte aligned: the codes
  *                   in the order in which the matrix cores take them (opaque)
  *   scales          pararnn_q4_scale_bytes() = G * H * dh / group * 2 bytes, device, 2-byte aligned: bf16,

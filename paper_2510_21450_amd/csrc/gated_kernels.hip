@@ -654,8 +654,12 @@ bool shape_of(int dtype, int B, int L, int H, int G, Shape *s)
     return true;
 }
 
-// Row offsets of a tile are 32-bit (128 steps x 3 gates x 4 bytes x 2^20 channels), tile numbers too.
-bool size_ok(const Shape &s, int H) { return H <= (1 << 20) && s.tiles < (1ll << 31) - 1; }
+// Row offsets of a tile are 32-bit (128 steps x 3 gates x 4 bytes x 2^20 channels), and so are the numbers of a launch's threads (512 of
+// a tile; one for each channel of a walk).
+bool size_ok(const Shape &s, int B, int H)
+{
+    return H <= (1 << 20) && s.tiles < (1ll << 23) && (long long)B * H < (1ll << 32) - 256;
+}
 
 // Whether rows can be taken n elements at a time
 bool rows_of(int n, int H, int dtype, std::initializer_list<const void *> ptrs)
@@ -722,13 +726,13 @@ template <typename T, int G> hipError_t launch_walk(const GatedArgs &a, bool pai
 
 // Control block and carry records for the call: cleared, unless the library knows what an earlier call left in this workspace.
 // False: a launch failed.
-bool take_workspace(void *workspace, const Shape &s, GatedArgs *a, hipStream_t st)
+bool take_workspace(void *workspace, const Shape &s, unsigned int spin_limit, GatedArgs *a, hipStream_t st)
 {
     char *ws = static_cast<char *>(workspace);
     a->ticket = reinterpret_cast<unsigned int *>(ws);
     a->rec = reinterpret_cast<word_t *>(ws + kCtrl);
     a->queues = (int)std::min<long long>(kQueues, s.chains);
-    a->spin_limit = kSpinLimit;
+    a->spin_limit = spin_limit;
     // FNV-1a; what the words are used for depends on the numbers of chains and tiles alone
     unsigned long long sig = 1469598103934665603ull;
     for (unsigned long long v : {0x6761746564ull, (unsigned long long)s.n_lt, (unsigned long long)s.chains})
@@ -750,17 +754,17 @@ bool misaligned(const void *p, size_t n) { return (uintptr_t)p % n != 0; }
 size_t gated_workspace_bytes(int dtype, int B, int L, int H, int G)
 {
     Shape s;
-    return shape_of(dtype, B, L, H, G, &s) && size_ok(s, H) ? s.bytes : 0;
+    return shape_of(dtype, B, L, H, G, &s) && size_ok(s, B, H) ? s.bytes : 0;
 }
 
 size_t gated_checkpoint_bytes(int dtype, int B, int L, int H, int G)
 {
     Shape s;
-    return shape_of(dtype, B, L, H, G, &s) && size_ok(s, H) ? (size_t)B * s.n_lt * H * sizeof(float) : 0;
+    return shape_of(dtype, B, L, H, G, &s) && size_ok(s, B, H) ? (size_t)B * s.n_lt * H * sizeof(float) : 0;
 }
 
 int gated_forward(int dtype, const void *u, const float *h0, const int *lengths, int B, int L, int H, int G, void *h,
-                  float *h_last, float *checkpoints, void *workspace, size_t workspace_bytes, hipStream_t st)
+                  float *h_last, float *checkpoints, void *workspace, size_t workspace_bytes, unsigned int spin_limit, hipStream_t st)
 {
     Shape s;
     if (!shape_of(dtype, B, L, H, G, &s) || !u || !h || (!workspace && s.n_lt > 1) || misaligned(workspace, 256)) return PARARNN_INVALID_ARG;
@@ -768,7 +772,7 @@ int gated_forward(int dtype, const void *u, const float *h0, const int *lengths,
     if (misaligned(u, es) || misaligned(h, es) || misaligned(h0, 4) || misaligned(lengths, 4) || misaligned(h_last, 4) ||
         misaligned(checkpoints, 4))
         return PARARNN_INVALID_ARG;
-    if (!size_ok(s, H)) return PARARNN_UNSUPPORTED;
+    if (!size_ok(s, B, H)) return PARARNN_UNSUPPORTED;
     if (s.n_lt > 1 && workspace_bytes < s.bytes) return PARARNN_WORKSPACE_TOO_SMALL;
     GatedArgs a = {};
     a.u = u; a.h0 = h0; a.lengths = lengths; a.h = h; a.last = h_last; a.ckpt = checkpoints;
@@ -779,7 +783,7 @@ int gated_forward(int dtype, const void *u, const float *h0, const int *lengths,
                                                    : (G == 2 ? launch_walk<float, 2>(a, pairs, st) : launch_walk<float, 3>(a, pairs, st));
         return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
     }
-    if (s.n_lt > 1 && !take_workspace(workspace, s, &a, st)) {
+    if (s.n_lt > 1 && !take_workspace(workspace, s, spin_limit, &a, st)) {
         workspace_forget(workspace);
         return PARARNN_HIP_ERROR;
     }
@@ -790,7 +794,7 @@ int gated_forward(int dtype, const void *u, const float *h0, const int *lengths,
 
 int gated_backward(int dtype, const void *u, const float *checkpoints, const int *lengths, const void *dL_dh,
                    const float *dL_dlast, int B, int L, int H, int G, void *dL_du, float *dL_dh0, void *workspace,
-                   size_t workspace_bytes, hipStream_t st)
+                   size_t workspace_bytes, unsigned int spin_limit, hipStream_t st)
 {
     Shape s;
     if (!shape_of(dtype, B, L, H, G, &s) || !u || !checkpoints || !dL_du || (!workspace && s.n_lt > 1) || misaligned(workspace, 256))
@@ -799,12 +803,12 @@ int gated_backward(int dtype, const void *u, const float *checkpoints, const int
     if (misaligned(u, es) || misaligned(dL_dh, es) || misaligned(dL_du, es) || misaligned(checkpoints, 4) || misaligned(lengths, 4) ||
         misaligned(dL_dlast, 4) || misaligned(dL_dh0, 4))
         return PARARNN_INVALID_ARG;
-    if (!size_ok(s, H)) return PARARNN_UNSUPPORTED;
+    if (!size_ok(s, B, H)) return PARARNN_UNSUPPORTED;
     if (s.n_lt > 1 && workspace_bytes < s.bytes) return PARARNN_WORKSPACE_TOO_SMALL;
     GatedArgs a = {};
     a.u = u; a.lengths = lengths; a.ckpt = const_cast<float *>(checkpoints); a.g = dL_dh; a.dlast = dL_dlast; a.du = dL_du; a.dh0 = dL_dh0;
     a.B = B; a.L = L; a.H = H; a.n_lt = s.n_lt; a.groups = s.groups; a.chains = (int)s.chains;
-    if (s.n_lt > 1 && !take_workspace(workspace, s, &a, st)) {
+    if (s.n_lt > 1 && !take_workspace(workspace, s, spin_limit, &a, st)) {
         workspace_forget(workspace);
         return PARARNN_HIP_ERROR;
     }

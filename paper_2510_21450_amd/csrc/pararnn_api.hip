@@ -608,7 +608,7 @@ int pararnn_gated_forward(int dtype, const void *u, const float *h0, const int *
                           float *h_last, float *checkpoints, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     return gated_forward(dtype, u, h0, lengths, B, L, H, G, h, h_last, checkpoints, workspace, workspace_bytes,
-                         static_cast<hipStream_t>(hip_stream));
+                         settings().spin_limit, static_cast<hipStream_t>(hip_stream));
 }
 
 int pararnn_gated_backward(int dtype, const void *u, const float *checkpoints, const int *lengths, const void *dL_dh,
@@ -616,7 +616,7 @@ int pararnn_gated_backward(int dtype, const void *u, const float *checkpoints, c
                            size_t workspace_bytes, void *hip_stream)
 {
     return gated_backward(dtype, u, checkpoints, lengths, dL_dh, dL_dlast, B, L, H, G, dL_du, dL_dh0, workspace, workspace_bytes,
-                          static_cast<hipStream_t>(hip_stream));
+                          settings().spin_limit, static_cast<hipStream_t>(hip_stream));
 }
 
 size_t pararnn_q4_packed_bytes(int H, int G, int n_heads) { return q4_packed_bytes(H, G, n_heads); }

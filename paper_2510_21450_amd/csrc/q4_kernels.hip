@@ -243,9 +243,10 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
     extern __shared__ __align__(16) float s_red[];
     const int lane = threadIdx.x & 63, n = lane & 15, kq = lane >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int W = blockDim.x >> 6;
-    const int per_gate = a.tiles / CT;
-    const int g0 = STEP ? 0 : (int)blockIdx.x / per_gate, ct = ((int)blockIdx.x - g0 * per_gate) * CT;
-    const int m0 = (int)blockIdx.y * 16 * MT;
+    const unsigned int per_gate = a.tiles / CT, all = STEP ? per_gate : per_gate * a.G;
+    const unsigned int mb = blockIdx.x / all, tile = blockIdx.x - mb * all;
+    const int g0 = STEP ? 0 : (int)(tile / per_gate), ct = (int)(tile - g0 * per_gate) * CT;
+    const int m0 = (int)mb * 16 * MT;
     const int head = ct * 16 / a.dh;                         // (a multiple of 64 channels: the CT tiles are of one head)
     // bases that all lanes share, and 32-bit offsets from them.  Rows behind the last are read as the block's first: a row of x
     // reaches that row's sums alone, and those are not written.
@@ -437,27 +438,28 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
 }
 
 // ------------------------------------------------------------------ host
-// Rows up to which bf16 inputs take q4_rows_kernel, beyond the weights are written out in bf16 for the tiles of the projection.  The
-// former does 0.3 PFLOP/s; the latter up to 1, but a tile of 128 x 128 takes 0.026 us for each input of a head whatever there
-// is beside it.  (H x gates, dh): rows at which both take the same and what that is, from 65 to 2048 rows measured: (2048 x 2, 2048)
-// 1050, 57 us; (4096 x 3, 1024) 340, 42; (8192 x 2, 1024) 270, 44; (2048 x 3, 1024) 660, 38; (1024 x 3, 256) 1100, 17;
-// (512 x 2, 256) beyond 2048.  At 128 rows: 9 us to 56, 20 to 41, 20 to 44, 11 to 35, 5.5 to 15, 3.3 to 14.
+// Rows up to which bf16 inputs take q4_rows_kernel; beyond, the weights are written out in bf16 for the tiles of the projection.  The
+// former's rate grows with the inputs of a head (its workgroups' starts and sums): 0.13 PFLOP/s for 256 of them, 0.2 for 512, 0.28
+// for 1024, 0.36 for 2048; the latter takes 9 us and 0.022 for each input of a head longer to start with, whatever the rows, and
+// then does up to 1.  (H x gates, dh): rows at which both took the same, from 128 to 4096 rows measured, and the time: (2048 x 2, 2048)
+// 1280, 57 us; (4096 x 3, 1024) 400, 42; (8192 x 2, 1024) 350, 45; (2048 x 3, 1024) 720, 38; (512 x 4, 512) 1750, 23; (1536 x 2, 384)
+// 1200, 21; (1024 x 3, 256) 1100, 18; (512 x 2, 256), (256 x 3, 64) and (64 x 2, 64) beyond 4096.  At 128 rows: 8 us to 56, 17 to 41,
+// 17 to 44, 9 to 33, 4 to 19, 6 to 17, 5 to 15, 3 to 14.
 int exact_rows(int H, int G, int n_heads)
 {
-    const double dh = H / n_heads, rows = (0.5 + 0.026 * dh) * 0.13e9 / ((double)G * H * dh);
-    return rows < 64 ? 64 : rows > 1e6 ? 1000000 : (int)rows;
+    const double dh = H / n_heads, rate = 0.48 * dh / (dh + 700.0);
+    const double rows = (9.0 + 0.022 * dh) * 1e9 / (2.0 * G * H * dh * (1.0 / rate - 0.3));
+    return rows < 64.0 ? 64 : rows > 1e6 ? 1000000 : (int)rows;
 }
-constexpr int kWorkgroups = 192;        // fewer leave too much of the device idle
-
-
 bool weights_ok(int H, int G, int n_heads) { return H >= 1 && G >= 1 && G <= 8 && n_heads >= 1 && H % n_heads == 0; }
 bool group_ok(int group) { return group == 32 || group == 64 || group == 128; }
-// what the kernels have no form for (2^38 weights a gate: workgroups are numbered in 32 bits)
-bool unsupported(int H, int n_heads, int group)
+// what the kernels have no form for (6e10 weights: the threads of a launch are numbered in 32 bits, 16 weights each)
+bool unsupported(int H, int G, int n_heads, int group)
 {
     const int dh = H / n_heads;
-    return H > (1 << 20) || dh % 64 || dh % group || (double)H * dh > 2.7e11;
+    return H > (1 << 20) || dh % 64 || dh % group || (double)G * H * dh > 6e10;
 }
+int status_of(hipError_t e) { return e == hipSuccess ? PARARNN_OK : e == hipErrorInvalidConfiguration ? PARARNN_UNSUPPORTED : PARARNN_HIP_ERROR; }
 bool misaligned(const void *p, size_t n) { return (uintptr_t)p % n != 0; }
 
 PrepArgs prep_args(int H, int G, int n_heads, int group, int per)
@@ -479,7 +481,9 @@ template <typename T, int MT, int NG, int CT, bool STEP> hipError_t launch_rows(
     const int held = sums_in_lds(NG * CT * MT);
     if (W > held)                                             // they are halved until they fit
         while (W & (W - 1)) --W;
-    const dim3 grid((unsigned)(a.tiles / CT) * (STEP ? 1 : a.G), (unsigned)((a.rows + 16 * MT - 1) / (16 * MT))), block(64 * W);
+    const long long blocks = (long long)(a.tiles / CT) * (STEP ? 1 : a.G) * ((a.rows + 16 * MT - 1) / (16 * MT));
+    if (blocks * 512 >= (1ll << 32)) return hipErrorInvalidConfiguration;      // threads of a launch are numbered in 32 bits
+    const dim3 grid((unsigned)blocks), block(64 * W);
     const size_t sums = (size_t)(W > held ? std::max(W / 2, held) : W) * NG * CT * MT * 1024;
     const size_t lds = MT == 1 ? sums : std::max(sums, (size_t)W * MT * 16 * 64 * sizeof(T));
     if constexpr (MT < 4)
@@ -490,13 +494,14 @@ template <typename T, int MT, int NG, int CT, bool STEP> hipError_t launch_rows(
     hipLaunchKernelGGL((q4_rows_kernel<T, MT, NG, CT, STEP, false>), grid, block, lds, st, a);
     return hipGetLastError();
 }
+constexpr int kWorkgroups = 192;        // fewer leave too much of the device idle
 // Rows and channels of a workgroup: the more, the fewer times weights and inputs are read, as long as there are workgroups for the
 // device.  bf16, up to 16 rows, 16 x 16 against 32 x 64 (a step: 32 x 16 of each gate): 3 x 4096 x 4096 weights 15.2 to 19.9 us -> 11.7;
 // a step with 2 x 8192 x 1024 6.1 to 7.0 -> 5.5, with 2 x 4096 x 4096 8.6 to 9.8 -> 8.5 to 8.7; fewer workgroups lose, 3 x 2048 x 1024
 // 3.5 -> 5.3.  fp32, whose terms cost more than the weights, only gains beyond 16 rows.
 template <typename T, int NG, bool STEP> hipError_t launch_rows_of(RowsQ4Args a, int n_heads, int group, hipStream_t st)
 {
-    a.dh = a.H / n_heads; a.nu = a.dh / 64; a.ng = a.dh / group; a.tiles = a.H / 16;
+    a.dh = a.H / n_heads; a.nu = a.dh / 64; a.ng = a.dh / group; a.tiles = (unsigned)a.H / 16;
     a.unit_shift = group == 128 ? 1 : 0;
     const long long tiles = (long long)a.tiles * (STEP ? 1 : a.G);
     auto enough = [&](int mt, int ct) { return tiles / ct * ((a.rows + 16 * mt - 1) / (16 * mt)) >= kWorkgroups; };
@@ -514,13 +519,13 @@ template <typename T, int NG, bool STEP> hipError_t launch_rows_of(RowsQ4Args a,
 
 size_t q4_packed_bytes(int H, int G, int n_heads)
 {
-    if (!weights_ok(H, G, n_heads) || unsupported(H, n_heads, 32)) return 0;
+    if (!weights_ok(H, G, n_heads) || unsupported(H, G, n_heads, 32)) return 0;
     return (size_t)G * H * (H / n_heads) / 2;
 }
 
 size_t q4_scale_bytes(int H, int G, int n_heads, int group)
 {
-    if (!weights_ok(H, G, n_heads) || !group_ok(group) || unsupported(H, n_heads, group)) return 0;
+    if (!weights_ok(H, G, n_heads) || !group_ok(group) || unsupported(H, G, n_heads, group)) return 0;
     return (size_t)G * H * (H / n_heads / group) * 2;
 }
 
@@ -529,7 +534,7 @@ int q4_quantize(const float *Wx, int H, int G, int n_heads, int group, void *pac
     if (!weights_ok(H, G, n_heads) || !group_ok(group) || !Wx || !packed || !scales || misaligned(Wx, 4) || misaligned(packed, 16) ||
         misaligned(scales, 2))
         return PARARNN_INVALID_ARG;
-    if (unsupported(H, n_heads, group)) return PARARNN_UNSUPPORTED;
+    if (unsupported(H, G, n_heads, group)) return PARARNN_UNSUPPORTED;
     PrepArgs a = prep_args(H, G, n_heads, group, group == 128 ? 2 : 1);
     a.W = Wx; a.packed_out = static_cast<u2v *>(packed); a.scales_out = static_cast<unsigned short *>(scales);
     if (group == 128) hipLaunchKernelGGL(q4_quantize_kernel<2>, prep_grid(a, H, G), prep_block(a), 0, st, a);
@@ -543,7 +548,7 @@ int q4_pack(const signed char *codes, const void *code_scales, int H, int G, int
     if (!weights_ok(H, G, n_heads) || !group_ok(group) || !codes || !code_scales || !packed || !scales || misaligned(code_scales, 2) ||
         misaligned(packed, 16) || misaligned(scales, 2))
         return PARARNN_INVALID_ARG;
-    if (unsupported(H, n_heads, group)) return PARARNN_UNSUPPORTED;
+    if (unsupported(H, G, n_heads, group)) return PARARNN_UNSUPPORTED;
     PrepArgs a = prep_args(H, G, n_heads, group, 1);
     a.codes = codes; a.code_scales = static_cast<const unsigned short *>(code_scales);
     a.packed_out = static_cast<u2v *>(packed); a.scales_out = static_cast<unsigned short *>(scales);
@@ -556,7 +561,7 @@ int q4_dequantize(const void *packed, const void *scales, int H, int G, int n_he
     if (!weights_ok(H, G, n_heads) || !group_ok(group) || !packed || !scales || !Wx || misaligned(packed, 16) || misaligned(scales, 2) ||
         misaligned(Wx, 4))
         return PARARNN_INVALID_ARG;
-    if (unsupported(H, n_heads, group)) return PARARNN_UNSUPPORTED;
+    if (unsupported(H, G, n_heads, group)) return PARARNN_UNSUPPORTED;
     PrepArgs a = prep_args(H, G, n_heads, group, 1);
     a.packed = static_cast<const u2v *>(packed); a.scales = static_cast<const unsigned short *>(scales); a.W_out = Wx;
     hipLaunchKernelGGL(q4_dequantize_kernel<false>, prep_grid(a, H, G), prep_block(a), 0, st, a);
@@ -565,7 +570,7 @@ int q4_dequantize(const void *packed, const void *scales, int H, int G, int n_he
 
 int q4_exact_rows(int H, int G, int n_heads)
 {
-    return weights_ok(H, G, n_heads) && !unsupported(H, n_heads, 32) ? exact_rows(H, G, n_heads) : -1;
+    return weights_ok(H, G, n_heads) && !unsupported(H, G, n_heads, 32) ? exact_rows(H, G, n_heads) : -1;
 }
 
 size_t q4_workspace_bytes(int dtype, int B, int L, int H, int G, int n_heads, int group)
@@ -583,7 +588,7 @@ int q4_project(int dtype, const void *x, const void *packed, const void *scales,
         !packed || !scales || !u || !workspace || misaligned(x, 16) || misaligned(packed, 16) || misaligned(scales, 2) ||
         misaligned(bias, 4) || misaligned(u, es) || misaligned(workspace, 256))
         return PARARNN_INVALID_ARG;
-    if (unsupported(H, n_heads, group)) return PARARNN_UNSUPPORTED;
+    if (unsupported(H, G, n_heads, group)) return PARARNN_UNSUPPORTED;
     const size_t need = q4_workspace_bytes(dtype, B, L, H, G, n_heads, group);
     if (need == 0) return PARARNN_INVALID_ARG;
     if (workspace_bytes < need) return PARARNN_WORKSPACE_TOO_SMALL;
@@ -603,7 +608,7 @@ int q4_project(int dtype, const void *x, const void *packed, const void *scales,
     a.x = x; a.packed = static_cast<const u2v *>(packed); a.scales = static_cast<const unsigned short *>(scales); a.bias = bias; a.out = u;
     a.rows = rows; a.H = H; a.G = G;
     const hipError_t e = dtype == PARARNN_BF16 ? launch_rows_of<unsigned short, 1, false>(a, n_heads, group, st) : launch_rows_of<float, 1, false>(a, n_heads, group, st);
-    return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
+    return status_of(e);
 }
 
 int q4_step(int dtype, const void *x, const void *packed, const void *scales, const float *bias, const float *h, int B, int H, int G,
@@ -614,7 +619,7 @@ int q4_step(int dtype, const void *x, const void *packed, const void *scales, co
         !x || !packed || !scales || !y || !h_next || misaligned(x, 16) || misaligned(packed, 16) || misaligned(scales, 2) ||
         misaligned(bias, 4) || misaligned(h, 4) || misaligned(h_next, 4) || misaligned(y, es))
         return PARARNN_INVALID_ARG;
-    if (unsupported(H, n_heads, group) || B > (1 << 20)) return PARARNN_UNSUPPORTED;
+    if (unsupported(H, G, n_heads, group) || B > (1 << 20)) return PARARNN_UNSUPPORTED;
     RowsQ4Args a = {};
     a.x = x; a.packed = static_cast<const u2v *>(packed); a.scales = static_cast<const unsigned short *>(scales); a.bias = bias; a.h = h;
     a.out = y; a.h_next = h_next;
@@ -622,7 +627,7 @@ int q4_step(int dtype, const void *x, const void *packed, const void *scales, co
     const hipError_t e = dtype == PARARNN_BF16
                              ? (G == 2 ? launch_rows_of<unsigned short, 2, true>(a, n_heads, group, st) : launch_rows_of<unsigned short, 3, true>(a, n_heads, group, st))
                              : (G == 2 ? launch_rows_of<float, 2, true>(a, n_heads, group, st) : launch_rows_of<float, 3, true>(a, n_heads, group, st));
-    return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
+    return status_of(e);
 }
 
 }  // namespace pararnn

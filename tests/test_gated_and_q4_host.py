@@ -60,6 +60,9 @@ def test_gated_refusals(lib):
                    dict(u=A + 2), dict(lengths=A + 2)):
             assert call(**kw) == INVALID, (call, kw)
         assert call(H=(1 << 20) + 1) == UNSUPPORTED
+        # more tiles, or channels of all sequences, than a launch has threads for
+        assert call(B=1 << 23, L=1, H=64, bytes=1 << 60) == UNSUPPORTED and call(B=1 << 14, L=129 << 10, H=1, bytes=1 << 60) == UNSUPPORTED
+        assert call(B=1 << 13, L=1, H=1 << 20, bytes=1 << 60) == UNSUPPORTED
         assert call(bytes=lib.pararnn_gated_workspace_bytes(F32, 2, 300, 64, 2) - 1) == TOO_SMALL
         assert call(dtype=BF16, u=A + 1) == INVALID
     for kw in (dict(h=None), dict(h=A + 2), dict(h0=A + 2), dict(last=A + 2), dict(ck=A + 2)):
@@ -102,7 +105,7 @@ def test_q4_refusals(lib):
         for kw in (dict(packed=None), dict(packed=A + 8), dict(scales=None), dict(scales=A + 1), dict(H=0), dict(G=0), dict(G=9),
                    dict(heads=0), dict(heads=3), dict(group=0), dict(group=96)):
             assert call(**kw) == INVALID, (call, kw)
-        for kw in (dict(H=96), dict(H=192, group=128), dict(H=1 << 21, heads=1 << 14, group=32)):
+        for kw in (dict(H=96), dict(H=192, group=128), dict(H=1 << 21, heads=1 << 14, group=32), dict(H=1 << 18, G=3)):
             assert call(**kw) == UNSUPPORTED, (call, kw)
     for call in (quantize, pack, dequantize):
         assert call(W=None) == INVALID
@@ -114,6 +117,7 @@ def test_q4_refusals(lib):
     many = lib.pararnn_q4_exact_rows(128, 2, 1) + 1
     assert project(dtype=BF16, B=1, L=many, bytes=256) == TOO_SMALL and project(dtype=BF16, B=1, L=many, u=A + 2) == UNSUPPORTED
     assert step(G=1) == INVALID and step(G=4) == INVALID and step(y=None) == INVALID and step(nxt=None) == INVALID
+    assert project(B=1 << 10, L=1 << 19, H=1 << 14, heads=1 << 8) == UNSUPPORTED        # more workgroups than a launch has
     assert step(h=A + 2) == INVALID and step(nxt=A + 2) == INVALID and step(B=(1 << 20) + 1) == UNSUPPORTED
 
 

@@ -170,6 +170,47 @@ def test_same_bits_every_time(P):
         assert all(torch.equal(a, b) for a, b in zip(first, got))
 
 
+def both(P, u, h0, g, d, **kw):
+    h, last, ckpt = P.gated_forward(u, h0, checkpoints=True, **kw)
+    return (h, last, ckpt) + tuple(P.gated_backward(u, ckpt, g, d, **kw))
+
+
+def test_workspaces_of_any_content(P):
+    """A workspace that holds anything, records of earlier calls among it, with and without the promise that nothing else writes to
+    it; calls of different sizes and both directions on the same one."""
+    cases = [[cuda(t) for t in problem(2, L, H, 2, torch.float32, seed=L)] for L, H in ((900, 130), (400, 64), (3000, 64))]
+    want = [both(P, *c) for c in cases]
+    size = max(P.gated_workspace_bytes(torch.float32, 2, c[0].shape[1], c[0].shape[3], 2) for c in cases)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    try:
+        for reuse in (False, True):
+            P.set_workspace_reuse(reuse)
+            ws.random_(0, 256, generator=torch.Generator("cuda").manual_seed(1))
+            if reuse:
+                both(P, *cases[0], workspace=torch.empty_like(ws))       # another address: what is known of it is not known of ws
+            for k in (0, 0, 1, 0, 2, 2, 1, 0):
+                assert all(torch.equal(a, b) for a, b in zip(want[k], both(P, *cases[k], workspace=ws))), (reuse, k)
+    finally:
+        P.set_workspace_reuse(False)
+
+
+def test_a_wait_that_runs_out(P):
+    """One poll of a neighbour instead of millions: every workgroup still ends, what it did not get is NaN, and later calls on the same
+    workspace are right again."""
+    c = [cuda(t) for t in problem(1, 30000, 64, 2, torch.float32, seed=17)]
+    want = both(P, *c)
+    try:
+        P.set_spin_limit(1)
+        got = both(P, *c)
+        torch.cuda.synchronize()
+    finally:
+        P.set_spin_limit(0)
+    ok = (got[0] == want[0]) | torch.isnan(got[0])
+    assert ok.all()
+    again = both(P, *c)
+    assert all(torch.equal(a, b) for a, b in zip(want, again))
+
+
 def scan_of_channels(u, h0):
     """64-bit states of a few channels of a long sequence on the GPU, by doubling."""
     f, i, v = ref.gates(u.double())
