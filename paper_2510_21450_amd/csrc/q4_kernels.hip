@@ -248,7 +248,7 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
     const int g0 = STEP ? 0 : (int)(tile / per_gate), ct = (int)(tile - g0 * per_gate) * CT;
     const int m0 = (int)mb * 16 * MT;
     const int head = ct * 16 / a.dh;                         // (a multiple of 64 channels: the CT tiles are of one head)
-    // bases that all lanes share, and 32-bit offsets from them.  Rows behind the last are read as the block's first: a row of x
+    // bases that all lanes share and scalar registers hold, and 32-bit offsets from them: no address arithmetic for a load.  Rows behind the last are read as the block's first: a row of x
     // reaches that row's sums alone, and those are not written.
     const T *x = static_cast<const T *>(a.x) + (size_t)m0 * a.H + (size_t)head * a.dh;
     auto weights = [&](int g) { return a.packed + ((size_t)(g0 + g / CT) * a.tiles + ct + g % CT) * a.nu * 64; };
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
         first_h = a.h[(size_t)row_of(threadIdx.x) * a.H + channel_of(threadIdx.x)];
 
     // one unit's products; x(m, s): the eight inputs of 16 rows m at step s that this lane multiplies
-    auto multiply = [&](const u2v (&q)[NT], const unsigned short (&sc)[NT][2], auto &&x_at) {
+    auto multiply = [&](const u2v (&q)[NT], const unsigned int (&sc)[NT][2], auto &&x_at) {
         constexpr int PARTS = G32 ? 2 : 1, STEPS = 2 / PARTS;             // groups of a unit, steps of 32 inputs in each
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
                 bf8v b[STEPS];
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s) b[s] = TERMS == 1 ? operand(q[g][p * STEPS + s]) : operand_signed(q[g][p * STEPS + s]);
-                const float scale = bf16_to_f32(sc[g][p]);
+                const float scale = __uint_as_float(sc[g][p] << 16);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     f4v acc = start[m];
@@ -307,16 +307,13 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
             }
         }
     };
-    auto load_weights = [&](int ku, u2v (&q)[NT], unsigned short (&sc)[NT][2]) {
+    auto load_weights = [&](int ku, u2v (&q)[NT], unsigned int (&sc)[NT][2]) {
 #pragma unroll
         for (int g = 0; g < NT; ++g) {
-            q[g] = weights(g)[ku * 64 + lane];
-            if constexpr (G32) {
-                sc[g][0] = scales(g)[2 * ku * 16 + n];
-                sc[g][1] = scales(g)[(2 * ku + 1) * 16 + n];
-            } else {
-                sc[g][0] = scales(g)[(ku >> a.unit_shift) * 16 + n];
-            }
+            q[g] = (weights(g) + (size_t)ku * 64)[(unsigned)lane];
+            const unsigned short *s = scales(g) + (size_t)(G32 ? 2 * ku : ku >> a.unit_shift) * 16;
+            sc[g][0] = s[(unsigned)n];
+            if constexpr (G32) sc[g][1] = s[16u + (unsigned)n];
         }
     };
     if constexpr (MT == 1) {
@@ -324,7 +321,7 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
         const unsigned int at = row_at(n) + 8 * kq;
         for (int base = w; base < a.nu; base += W * U) {
             u2v q[U][NT];
-            unsigned short sc[U][NT][2];
+            unsigned int sc[U][NT][2];            // (whole registers: halves would be put together, one load waiting for the other)
             Eight<T> xr[U][2];
 #pragma unroll
             for (int i = 0; i < U; ++i) {
@@ -332,7 +329,7 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
                 if (ku >= a.nu) break;
                 load_weights(ku, q[i], sc[i]);
 #pragma unroll
-                for (int s = 0; s < 2; ++s) xr[i][s].load(x + (at + (unsigned int)(ku * 64 + 32 * s)));
+                for (int s = 0; s < 2; ++s) xr[i][s].load((x + (size_t)ku * 64 + 32 * s) + at);
             }
 #pragma unroll
             for (int i = 0; i < U; ++i) {
@@ -355,10 +352,10 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
         }
         u4v raw[LOADS];
         u2v q[NT], q_next[NT];
-        unsigned short sc[NT][2], sc_next[NT][2];
+        unsigned int sc[NT][2], sc_next[NT][2];
         auto load = [&](int ku) {
 #pragma unroll
-            for (int j = 0; j < LOADS; ++j) raw[j] = *reinterpret_cast<const u4v *>(x + (from[j] + (unsigned int)ku * 64));
+            for (int j = 0; j < LOADS; ++j) raw[j] = *reinterpret_cast<const u4v *>((x + (size_t)ku * 64) + from[j]);
             load_weights(ku, q_next, sc_next);
         };
         if (w < a.nu) load(w);
@@ -496,9 +493,10 @@ template <typename T, int MT, int NG, int CT, bool STEP> hipError_t launch_rows(
 }
 constexpr int kWorkgroups = 192;        // fewer leave too much of the device idle
 // Rows and channels of a workgroup: the more, the fewer times weights and inputs are read, as long as there are workgroups for the
-// device.  bf16, up to 16 rows, 16 x 16 against 32 x 64 (a step: 32 x 16 of each gate): 3 x 4096 x 4096 weights 15.2 to 19.9 us -> 11.7;
-// a step with 2 x 8192 x 1024 6.1 to 7.0 -> 5.5, with 2 x 4096 x 4096 8.6 to 9.8 -> 8.5 to 8.7; fewer workgroups lose, 3 x 2048 x 1024
-// 3.5 -> 5.3.  fp32, whose terms cost more than the weights, only gains beyond 16 rows.
+// device.  bf16, 16 x 16 against 32 x 64 (a step: 32 x 16 of each gate): with 3 x 4096 x 4096 weights 11.1 us for one row and 16.1
+// for 16 against 11.8 and 12.0; a step with 2 x 8192 x 1024 5.7 and 6.9 against 5.6 and 5.7, with 2 x 4096 x 4096 7.3 and 9.3 against
+// 8.5 and 8.6; with too few workgroups, 3 x 2048 x 1024, 3.4 and 4.4 against 5.4 and 5.5.  fp32, whose terms cost more than the
+// weights: 21 and 27 against 24 and 24, 5.0 and 6.6 against 8.8 and 8.9.
 template <typename T, int NG, bool STEP> hipError_t launch_rows_of(RowsQ4Args a, int n_heads, int group, hipStream_t st)
 {
     a.dh = a.H / n_heads; a.nu = a.dh / 64; a.ng = a.dh / group; a.tiles = (unsigned)a.H / 16;
@@ -510,7 +508,7 @@ template <typename T, int NG, bool STEP> hipError_t launch_rows_of(RowsQ4Args a,
     // (groups of 32, and three terms of fp32, leave no registers for 64 rows)
     if constexpr (bf16)
         if (group != 32 && a.rows > 32 && enough(4, C4)) return launch_rows<T, 4, NG, C4, STEP>(a, group, st);
-    if ((bf16 || a.rows > 16) && enough(2, C4)) return launch_rows<T, 2, NG, C4, STEP>(a, group, st);
+    if (a.rows > (bf16 ? 8 : 16) && enough(2, C4)) return launch_rows<T, 2, NG, C4, STEP>(a, group, st);
     if (a.rows > 16 && enough(2, 1)) return launch_rows<T, 2, NG, 1, STEP>(a, group, st);
     return launch_rows<T, 1, NG, 1, STEP>(a, group, st);
 }
