@@ -263,18 +263,31 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
 #pragma unroll
         for (int m = 0; m < MT; ++m) total[g][m] = f4v{0, 0, 0, 0};
 
-    // sum id = ((tile of channels, 16 rows), row & 3, lane) of this workgroup, below: a lane's channels are n of every tile
-    auto row_of = [&](int id) { return m0 + 16 * (id / 256 % MT) + 4 * kq + id / 64 % 4; };
-    auto channel_of = [&](int id) { return (ct + id / (256 * MT)) * 16 + n; };
-    float bias[NT], first_h = 0.0f;
+    // A lane's four sums of a tile, rows 4 kq .. 4 kq + 3 of channel n, lie together.  A thread finishes PER of them at a time: all four
+    // where there are tiles for every thread, else one (a step of 48 rows: 3.9 us to 4.4).
+    constexpr int PER = CT * MT >= 4 ? 4 : 1;
+    auto place = [&](int id, int *c, int *m, int *j) {       // tile of channels, of rows, first of the sums; returns the channel
+        *j = PER == 4 ? 0 : id / 64 % 4;
+        const int quad = id / (64 * (4 / PER));
+        *c = quad / MT;
+        *m = quad % MT;
+        return (ct + *c) * 16 + n;
+    };
+    constexpr int PLACES = CT * MT * 64 * (4 / PER);
+    float bias[NT], first_h[PER];
 #pragma unroll
     for (int g = 0; g < NT; ++g) bias[g] = a.bias ? a.bias[(size_t)(g0 + g / CT) * a.H + (ct + g % CT) * 16 + n] : 0.0f;
-    if (STEP && a.h && (int)threadIdx.x < CT * MT * 256 && row_of(threadIdx.x) < a.rows)
-        first_h = a.h[(size_t)row_of(threadIdx.x) * a.H + channel_of(threadIdx.x)];
+    if constexpr (STEP) {
+        int c, m, j;
+        const int ch = place(threadIdx.x, &c, &m, &j), row = m0 + 16 * m + 4 * kq + j;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) first_h[e] = a.h && (int)threadIdx.x < PLACES && row + e < a.rows ? a.h[(size_t)(row + e) * a.H + ch] : 0.0f;
+    }
 
     // one unit's products; x(m, s): the eight inputs of 16 rows m at step s that this lane multiplies
     auto multiply = [&](const u2v (&q)[NT], const unsigned int (&sc)[NT][2], auto &&x_at) {
-        constexpr int PARTS = G32 ? 2 : 1, STEPS = 2 / PARTS;             // groups of a unit, steps of 32 inputs in each
+        // parts of a unit: its groups; three terms of both steps at once would not fit the registers
+        constexpr int PARTS = G32 || TERMS == 3 ? 2 : 1, STEPS = 2 / PARTS;
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
             bf8v t[MT][STEPS][TERMS];
@@ -293,7 +306,7 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
                 bf8v b[STEPS];
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s) b[s] = TERMS == 1 ? operand(q[g][p * STEPS + s]) : operand_signed(q[g][p * STEPS + s]);
-                const float scale = __uint_as_float(sc[g][p] << 16);
+                const float scale = __uint_as_float(sc[g][G32 ? p : 0] << 16);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     f4v acc = start[m];
@@ -383,53 +396,67 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
         }
         __syncthreads();                                                  // the places are where the sums go
     }
-    // the waves' sums, in a fixed order; halves first while LDS does not hold those of all
+    // the waves' sums, in a fixed order; upper halves are added to the lower ones while LDS does not hold those of all
+    f4v *const red = reinterpret_cast<f4v *>(s_red) + lane;
     auto put = [&](int at) {
 #pragma unroll
         for (int g = 0; g < NT; ++g)
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s_red[((at * NT + g) * MT + m) * 256 + j * 64 + lane] = total[g][m][j];
+            for (int m = 0; m < MT; ++m) red[((at * NT + g) * MT + m) * 64] = total[g][m];
     };
-    for (; W > sums_in_lds(NT * MT); W /= 2) {
-        if (w >= W / 2 && w < W) put(w - W / 2);
+    while (W > sums_in_lds(NT * MT)) {
+        const int half = (W + 1) / 2;
+        if (w >= half && w < W) put(w - half);
         __syncthreads();
-        if (w < W / 2)
+        if (w < W - half)
 #pragma unroll
             for (int g = 0; g < NT; ++g)
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) total[g][m][j] += s_red[((w * NT + g) * MT + m) * 256 + j * 64 + lane];
+                for (int m = 0; m < MT; ++m) total[g][m] += red[((w * NT + g) * MT + m) * 64];
         __syncthreads();
+        W = half;
     }
     if (w < W) put(w);
     __syncthreads();
-    for (int id = threadIdx.x; id < CT * MT * 256; id += blockDim.x) {
-        const int row = row_of(id), ch = channel_of(id), c = id / (256 * MT);
+    for (int id = threadIdx.x; id < PLACES; id += blockDim.x) {
+        int c, m, j;
+        const int ch = place(id, &c, &m, &j), row = m0 + 16 * m + 4 * kq + j;
         if (row >= a.rows) continue;
-        float u[NG];
+        float u[NG][PER];
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            float sum = bias[g * CT];
+            float b = bias[g * CT];
 #pragma unroll
-            for (int k = 1; k < CT; ++k) sum = c == k ? bias[g * CT + k] : sum;
-            for (int p = 0; p < W; ++p) sum += s_red[(p * NT + g * CT) * MT * 256 + id];
-            u[g] = sum;
+            for (int k = 1; k < CT; ++k) b = c == k ? bias[g * CT + k] : b;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) u[g][e] = b;
+            for (int p = 0; p < W; ++p) {
+                const f4v *at = red + ((p * NT + g * CT + c) * MT + m) * 64;
+                if constexpr (PER == 4) {
+                    const f4v v = *at;
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) u[g][e] += v[e];
+                } else {
+                    u[g][0] += reinterpret_cast<const float *>(at)[j];
+                }
+            }
         }
-        if constexpr (STEP) {
-            const size_t at = (size_t)row * a.H + ch;
-            const float h = id == (int)threadIdx.x ? first_h : a.h ? a.h[at] : 0.0f;
-            const float f = fast_sigmoid(u[0]), i = fast_sigmoid(NG == 2 ? -u[0] : u[NG - 2]);
-            const float next = fmaf(f, h, i * u[NG - 1]);
-            a.h_next[at] = next;
-            if constexpr (sizeof(T) == 4) static_cast<float *>(a.out)[at] = next;
-            else static_cast<unsigned short *>(a.out)[at] = f32_to_bf16(next);
-        } else {
-            const size_t at = ((size_t)row * a.G + g0) * a.H + ch;
-            if constexpr (sizeof(T) == 4) static_cast<float *>(a.out)[at] = u[0];
-            else static_cast<unsigned short *>(a.out)[at] = f32_to_bf16(u[0]);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            if (row + e >= a.rows) break;
+            float out = u[0][e];
+            size_t at;
+            if constexpr (STEP) {
+                at = (size_t)(row + e) * a.H + ch;
+                const float h = id == (int)threadIdx.x ? first_h[e] : a.h ? a.h[at] : 0.0f;
+                const float f = fast_sigmoid(u[0][e]), i = fast_sigmoid(NG == 2 ? -u[0][e] : u[NG - 2][e]);
+                out = fmaf(f, h, i * u[NG - 1][e]);
+                a.h_next[at] = out;
+            } else {
+                at = ((size_t)(row + e) * a.G + g0) * a.H + ch;
+            }
+            if constexpr (sizeof(T) == 4) static_cast<float *>(a.out)[at] = out;
+            else static_cast<unsigned short *>(a.out)[at] = f32_to_bf16(out);
         }
     }
 }
@@ -474,21 +501,15 @@ dim3 prep_block(const PrepArgs &a) { return dim3(64 * (a.per_row < 4 ? a.per_row
 
 template <typename T, int MT, int NG, int CT, bool STEP> hipError_t launch_rows(const RowsQ4Args &a, int group, hipStream_t st)
 {
-    int W = a.nu < 8 ? a.nu : 8;
+    const int rounds = (a.nu + 7) / 8, W = (a.nu + rounds - 1) / rounds;       // waves with the same number of units, eight at most (64 KB of LDS)
     const int held = sums_in_lds(NG * CT * MT);
-    if (W > held)                                             // they are halved until they fit
-        while (W & (W - 1)) --W;
     const long long blocks = (long long)(a.tiles / CT) * (STEP ? 1 : a.G) * ((a.rows + 16 * MT - 1) / (16 * MT));
     if (blocks * 512 >= (1ll << 32)) return hipErrorInvalidConfiguration;      // threads of a launch are numbered in 32 bits
     const dim3 grid((unsigned)blocks), block(64 * W);
-    const size_t sums = (size_t)(W > held ? std::max(W / 2, held) : W) * NG * CT * MT * 1024;
+    const size_t sums = (size_t)std::min(W, held) * NG * CT * MT * 1024;
     const size_t lds = MT == 1 ? sums : std::max(sums, (size_t)W * MT * 16 * 64 * sizeof(T));
-    if constexpr (MT < 4)
-        if (group == 32) {
-            hipLaunchKernelGGL((q4_rows_kernel<T, MT, NG, CT, STEP, true>), grid, block, lds, st, a);
-            return hipGetLastError();
-        }
-    hipLaunchKernelGGL((q4_rows_kernel<T, MT, NG, CT, STEP, false>), grid, block, lds, st, a);
+    if (group == 32) hipLaunchKernelGGL((q4_rows_kernel<T, MT, NG, CT, STEP, true>), grid, block, lds, st, a);
+    else hipLaunchKernelGGL((q4_rows_kernel<T, MT, NG, CT, STEP, false>), grid, block, lds, st, a);
     return hipGetLastError();
 }
 constexpr int kWorkgroups = 192;        // fewer leave too much of the device idle
@@ -505,9 +526,9 @@ template <typename T, int NG, bool STEP> hipError_t launch_rows_of(RowsQ4Args a,
     auto enough = [&](int mt, int ct) { return tiles / ct * ((a.rows + 16 * mt - 1) / (16 * mt)) >= kWorkgroups; };
     constexpr int C4 = STEP ? 1 : 4;
     constexpr bool bf16 = sizeof(T) == 2;
-    // (groups of 32, and three terms of fp32, leave no registers for 64 rows)
+    // (three terms of fp32 leave no registers for 64 rows: 46 -> 88 us for 64 of 3 x 4096 x 4096)
     if constexpr (bf16)
-        if (group != 32 && a.rows > 32 && enough(4, C4)) return launch_rows<T, 4, NG, C4, STEP>(a, group, st);
+        if (a.rows > 32 && enough(4, C4)) return launch_rows<T, 4, NG, C4, STEP>(a, group, st);
     if (a.rows > (bf16 ? 8 : 16) && enough(2, C4)) return launch_rows<T, 2, NG, C4, STEP>(a, group, st);
     if (a.rows > 16 && enough(2, 1)) return launch_rows<T, 2, NG, 1, STEP>(a, group, st);
     return launch_rows<T, 1, NG, 1, STEP>(a, group, st);
