@@ -501,7 +501,7 @@ dim3 prep_block(const PrepArgs &a) { return dim3(64 * (a.per_row < 4 ? a.per_row
 
 template <typename T, int MT, int NG, int CT, bool STEP> hipError_t launch_rows(const RowsQ4Args &a, int group, hipStream_t st)
 {
-    const int rounds = (a.nu + 7) / 8, W = (a.nu + rounds - 1) / rounds;       // waves with the same number of units, eight at most (64 KB of LDS)
+    const int W = a.nu < 8 ? a.nu : 8;
     const int held = sums_in_lds(NG * CT * MT);
     const long long blocks = (long long)(a.tiles / CT) * (STEP ? 1 : a.G) * ((a.rows + 16 * MT - 1) / (16 * MT));
     if (blocks * 512 >= (1ll << 32)) return hipErrorInvalidConfiguration;      // threads of a launch are numbered in 32 bits
