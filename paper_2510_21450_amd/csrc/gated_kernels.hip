@@ -5,7 +5,7 @@
 //   adjoint  mu_t = f_t (g_t + mu_{t+1}) is the gradient of h_{t-1}, lam_t = g_t + mu_{t+1} that of h_t:
 //            du_v = lam i,  du_i = lam v i (1 - i),  du_f = lam h_{t-1} f (1 - f)  (G = 2: lam (h_{t-1} - v) f (1 - f))
 //
-// A tile is CW channels x TT steps of one sequence.  It is read from memory once: a thread takes VEC channels of C
+// A tile is CW channels x TT steps of one sequence (64 x 128 or 16 x 512).  It is read from memory once: a thread takes VEC channels of C
 // consecutive steps, 64 / LPR segments of a wave are joined by shuffles, the waves through LDS, the tiles along L by carry
 // records (look-back).  The forward pass leaves the fp32 state in front of every tile behind (checkpoints, 4 bytes a channel
 // for TT steps); the adjoint recomputes the states inside a tile from there, which reads 2 bytes a step and channel less than
@@ -24,8 +24,9 @@
 namespace pararnn {
 namespace {
 
-constexpr int kTT = 128;                 // steps of a tile
-constexpr int kCW = 64;                  // channels of a tile
+// Tiles: 64 channels x 128 steps, or 16 x 512 (narrow rows, and problems of few tiles); a single tile along L may be shorter
+constexpr int kWide = 64, kNarrow = 16;
+constexpr __host__ __device__ int tile_steps(int channels) { return 8192 / channels; }
 constexpr int kQueues = 16;              // counters that hand out tiles, kQueuePitch words apart (a line each)
 constexpr int kQueuePitch = 32;
 constexpr int kWaves = 8;                // of a tile's workgroup
@@ -126,46 +127,51 @@ __device__ __forceinline__ float value(word_t w) { return __uint_as_float((unsig
 
 // The values that enter tile lt from its neighbours in direction dir: the state behind the nearest tile that has one, carried through
 // the maps of those in between in the order and with the roundings those tiles themselves use, so that the result has the same
-// bits whichever tile that is.  The whole workgroup looks: wave w at the tile w + 1 steps away, a lane for each channel, so that W
-// tiles are asked in one trip to memory and no wave keeps more than one of them in registers.  Returns the number of maps
+// bits whichever tile that is.  The whole workgroup looks: wave w at the tile w + 1 steps away, a lane for each channel (or at the
+// next LK x 64 / CW tiles), so that W and more tiles are asked in one trip to memory and no wave keeps many of them in registers.  Returns the number of maps
 // between (the tiles found are in LDS then, carry_of() puts them together), or -1 when the wait ran out.
 // Tiles are numbered by a ticket in the order of their chain: every tile in front has been started by a workgroup that never
 // waits for this one, and the first of a chain publishes its state without waiting, so the wait ends.  A bound on the polls
 // ends it whatever happens; the result is then NaN.
-template <int W, int LK> struct Seen {          // LK: tiles that a wave looks at in one trip
-    float a[2][W * LK][kCW], s[2][W * LK][kCW];        // s: of a map, or the state behind the tile
-    int what[2][W * LK];                                  // 2: a state, 1: a map, 0: neither yet
+template <int W, int LK, int CW> struct Seen {
+    static constexpr int SUB = 64 / CW, N = W * LK * SUB;    // tiles that a wave looks at in one load; in one trip
+    static_assert(N <= 64, "");
+    float a[2][N][CW], s[2][N][CW];                          // s: of a map, or the state behind the tile
+    int what[2][N];                                          // 2: a state, 1: a map, 0: neither yet
 };
-template <int W, int LK>
-__device__ __forceinline__ int look_back(Seen<W, LK> &seen, const word_t *rec, int dir, int lt, int n_lt, bool active,
-                                                          unsigned int tag, unsigned int spin_limit, int *parity)
+// active: whether this lane's channel, lane % CW, is one of the tile's
+template <int W, int LK, int CW>
+__device__ __forceinline__ int look_back(Seen<W, LK, CW> &seen, const word_t *rec, int dir, int lt, int n_lt, bool active,
+                                         unsigned int tag, unsigned int spin_limit, int *parity)
 {
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int SUB = Seen<W, LK, CW>::SUB, N = Seen<W, LK, CW>::N;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sub = lane / CW, col = lane % CW;
     for (unsigned int spins = 0; spins < spin_limit; ++spins) {
         const int b = spins & 1;
         word_t x[LK], a[LK], s[LK];
         bool exists[LK];
 #pragma unroll
         for (int k = 0; k < LK; ++k) {
-            const int j = lt + (w * LK + k + 1) * dir;
+            const int j = lt + ((w * LK + k) * SUB + sub + 1) * dir;
             exists[k] = j >= 0 && j < n_lt;
-            const word_t *p = rec + (long long)(exists[k] ? j - lt : dir) * 3 * kCW + lane;      // lt + dir exists
-            x[k] = get(p + 2 * kCW);
+            const word_t *p = rec + (long long)(exists[k] ? j - lt : dir) * 3 * CW + col;      // lt + dir exists
+            x[k] = get(p + 2 * CW);
             a[k] = get(p);
-            s[k] = get(p + kCW);
+            s[k] = get(p + CW);
         }
 #pragma unroll
         for (int k = 0; k < LK; ++k) {
-            int what = 0;
-            if (exists[k]) what = __all(!active || has_tag(x[k], tag + 2)) ? 2 : __all(!active || (has_tag(a[k], tag + 1) && has_tag(s[k], tag + 1))) ? 1 : 0;
-            seen.a[b][w * LK + k][lane] = value(a[k]);
-            seen.s[b][w * LK + k][lane] = what == 2 ? value(x[k]) : value(s[k]);
-            if (lane == 0) seen.what[b][w * LK + k] = what;
+            // votes of the lanes that look at the same tile
+            auto all_of = [&](bool ok) { return (__ballot(!active || ok) >> (sub * CW) & (~0ull >> (64 - CW))) == ~0ull >> (64 - CW); };
+            const bool state = all_of(has_tag(x[k], tag + 2)), map = all_of(has_tag(a[k], tag + 1) && has_tag(s[k], tag + 1));
+            const int at = (w * LK + k) * SUB + sub;
+            seen.a[b][at][col] = value(a[k]);
+            seen.s[b][at][col] = state ? value(x[k]) : value(s[k]);
+            if (col == 0) seen.what[b][at] = !exists[k] ? 0 : state ? 2 : map ? 1 : 0;
         }
         __syncthreads();
         // (two buffers: a wave that goes on writes the other one, and is held by the next barrier until all have read this one)
-        static_assert(W * LK <= 64, "");
-        const int what = seen.what[b][lane % (W * LK)];
+        const int what = seen.what[b][lane % N];
         const unsigned long long states = __ballot(what == 2), gaps = __ballot(what == 0);
         if (states && (!gaps || __builtin_ctzll(states) < __builtin_ctzll(gaps))) {
             *parity = b;
@@ -175,19 +181,20 @@ __device__ __forceinline__ int look_back(Seen<W, LK> &seen, const word_t *rec, i
     }
     return -1;
 }
-// N channels from c on: what the look found
-template <int N, int W, int LK> __device__ __forceinline__ void carry_of(const Seen<W, LK> &seen, int found, int parity, int c, float (&v)[N])
+// K channels from c on: what the look found
+template <int K, int W, int LK, int CW>
+__device__ __forceinline__ void carry_of(const Seen<W, LK, CW> &seen, int found, int parity, int c, float (&v)[K])
 {
     if (found < 0) {
 #pragma unroll
-        for (int k = 0; k < N; ++k) v[k] = __uint_as_float(0x7fc00000u);
+        for (int k = 0; k < K; ++k) v[k] = __uint_as_float(0x7fc00000u);
         return;
     }
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = seen.s[parity][found][c + k];
+    for (int k = 0; k < K; ++k) v[k] = seen.s[parity][found][c + k];
     for (int q = found - 1; q >= 0; --q)
 #pragma unroll
-        for (int k = 0; k < N; ++k) v[k] = fmaf(seen.a[parity][q][c + k], v[k], seen.s[parity][q][c + k]);
+        for (int k = 0; k < K; ++k) v[k] = fmaf(seen.a[parity][q][c + k], v[k], seen.s[parity][q][c + k]);
 }
 
 struct GatedArgs {
@@ -202,7 +209,7 @@ struct GatedArgs {
     void *du;                     // backward: out
     float *dh0;                   // backward: out or NULL
     unsigned int *ticket;
-    word_t *rec;                  // [chain][tile][3][kCW]
+    word_t *rec;                  // [chain][tile][3][CW]
     unsigned int tag;             // of this call: aggregates carry tag + 1, states tag + 2
     unsigned int spin_limit;
     int B, L, H, n_lt, groups, chains, queues;
@@ -219,7 +226,6 @@ struct Place {
 // bounds a launch: its atomics take 12.5 ns each, 1.7 ms for 131072 tiles that move 6.4 GB.  Queue q's workgroups are
 // launched q, q + kQueues, ..., which are on one XCD, so that a line shared by two groups of channels is in its L2.
 // The last workgroup of a queue leaves the counter at zero for the next call.
-// TT: steps of a tile; kTT but where there is one along L.
 template <bool LOOK, bool REVERSE, int TT> __device__ __forceinline__ Place place_of(const GatedArgs &a, int *s_id)
 {
     Place p;
@@ -270,20 +276,20 @@ __device__ __forceinline__ unsigned int extent(int n, unsigned int row_bytes, un
     return n > 0 ? (unsigned int)n * row_bytes - first : 0u;
 }
 
-template <typename T, int G, int VEC, int W, int C, int LK>
+template <typename T, int G, int VEC, int CW, int W, int C, int LK>
 __global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a)
 {
-    constexpr int LPR = kCW / VEC, SEG = 64 / LPR;
+    constexpr int LPR = CW / VEC, SEG = 64 / LPR;
     constexpr int TT = W * SEG * C;
-    static_assert(LK == 0 || TT == kTT, "");
-    __shared__ float s_a[W][kCW], s_s[W][kCW], s_in[kCW];
+    static_assert(LK == 0 || TT == tile_steps(CW), "");
+    __shared__ float s_a[W][CW], s_s[W][CW], s_in[CW];
     constexpr bool LOOK = LK > 0;
-    __shared__ Seen<LOOK ? W : 1, LOOK ? LK : 1> s_seen;
+    __shared__ Seen<LOOK ? W : 1, LOOK ? LK : 1, CW> s_seen;
     __shared__ int s_id;
     const Place p = place_of<LOOK, false, TT>(a, &s_id);
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sg = lane / LPR, c0 = (lane % LPR) * VEC;
     const int t0 = (w * SEG + sg) * C;
-    const unsigned int es = sizeof(T), H = (unsigned int)a.H, first = (unsigned int)p.grp * kCW;
+    const unsigned int es = sizeof(T), H = (unsigned int)a.H, first = (unsigned int)p.grp * CW;
     const bool active = first + c0 < H;
     const unsigned int row_bytes = H * es, at_h = (active ? c0 * es : kOutside) + (unsigned int)t0 * row_bytes;
     const unsigned int at_u = at_h + (unsigned int)t0 * (G - 1) * row_bytes;
@@ -297,9 +303,9 @@ __global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a
         for (int g = 0; g < G; ++g)
             raw[j][g] = load_raw_at<T, VEC>(ru, at_u + (unsigned int)(j * G + g) * row_bytes);
 
-    const unsigned int ch = first + lane;                    // wave 0: a lane for each channel of the tile
-    const bool act = ch < H;
-    const float in0 = w == 0 && p.lt == 0 && act && a.h0 ? a.h0[(size_t)p.b * H + ch] : 0.0f;
+    const unsigned int ch = first + lane % CW;               // wave 0: a lane for each channel of the tile
+    const bool act = ch < H, one = lane < CW && act;
+    const float in0 = w == 0 && p.lt == 0 && one && a.h0 ? a.h0[(size_t)p.b * H + ch] : 0.0f;
 
     float f[C][VEC], b[C][VEC], A[VEC], S[VEC];
 #pragma unroll
@@ -342,7 +348,7 @@ __global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a
 #pragma unroll
         for (int k = 0; k < VEC; ++k) { A[k] = 1.0f; S[k] = 0.0f; }
     }
-    if (w == 0) s_in[lane] = in0;
+    if (w == 0 && lane < CW) s_in[lane] = in0;
     __syncthreads();
     // this wave's place among the waves
     float x[VEC], pa[VEC], ps[VEC];
@@ -352,12 +358,12 @@ __global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a
 #pragma unroll
         for (int k = 0; k < VEC; ++k) { ps[k] = fmaf(s_a[q][c0 + k], ps[k], s_s[q][c0 + k]); pa[k] *= s_a[q][c0 + k]; }
     const bool more = LOOK && p.lt + 1 < a.n_lt;
-    word_t *rec = a.rec + ((size_t)p.chain * a.n_lt + p.lt) * (3 * kCW);
+    word_t *rec = a.rec + ((size_t)p.chain * a.n_lt + p.lt) * (3 * CW);
     float ta = 1.0f, ts = 0.0f;
-    if (w == 0) {
+    if (w == 0 && lane < CW) {
 #pragma unroll
         for (int q = 0; q < W; ++q) { ts = fmaf(s_a[q][lane], ts, s_s[q][lane]); ta *= s_a[q][lane]; }
-        if (more && act && p.lt > 0) { put(rec + lane, ta, a.tag + 1); put(rec + kCW + lane, ts, a.tag + 1); }
+        if (more && act && p.lt > 0) { put(rec + lane, ta, a.tag + 1); put(rec + CW + lane, ts, a.tag + 1); }
     }
     int found = -1, parity = 0;
     if constexpr (LOOK)
@@ -368,11 +374,11 @@ __global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a
 #pragma unroll
         for (int k = 0; k < (int)(sizeof(v) / sizeof(v[0])); ++k) v[k] = s_in[c + k];
     };
-    if (w == 0 && act) {
+    if (w == 0 && one) {
         float in1[1];
         entering(lane, in1);
         const float in = in1[0], out = fmaf(ta, in, ts);
-        if (more) put(rec + 2 * kCW + lane, out, a.tag + 2);
+        if (more) put(rec + 2 * CW + lane, out, a.tag + 2);
         if (a.ckpt) a.ckpt[((size_t)p.b * a.n_lt + p.lt) * H + ch] = in;
         if (a.last && p.lt + 1 == a.n_lt) a.last[(size_t)p.b * H + ch] = out;      // (may be h0: read before the first state was published)
     }
@@ -395,20 +401,20 @@ __global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a
     }
 }
 
-template <typename T, int G, int VEC, int W, int C, int LK>
+template <typename T, int G, int VEC, int CW, int W, int C, int LK>
 __global__ __launch_bounds__(64 * W, 4) void gated_backward_kernel(const GatedArgs a)
 {
-    constexpr int LPR = kCW / VEC, SEG = 64 / LPR;
+    constexpr int LPR = CW / VEC, SEG = 64 / LPR;
     constexpr int TT = W * SEG * C;
-    static_assert(LK == 0 || TT == kTT, "");
-    __shared__ float s_a[W][kCW], s_s[W][kCW], s_m[W][kCW], s_in[kCW];
+    static_assert(LK == 0 || TT == tile_steps(CW), "");
+    __shared__ float s_a[W][CW], s_s[W][CW], s_m[W][CW], s_in[CW];
     constexpr bool LOOK = LK > 0;
-    __shared__ Seen<LOOK ? W : 1, LOOK ? LK : 1> s_seen;
+    __shared__ Seen<LOOK ? W : 1, LOOK ? LK : 1, CW> s_seen;
     __shared__ int s_id;
     const Place p = place_of<LOOK, true, TT>(a, &s_id);
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sg = lane / LPR, c0 = (lane % LPR) * VEC;
     const int t0 = (w * SEG + sg) * C;
-    const unsigned int es = sizeof(T), H = (unsigned int)a.H, first = (unsigned int)p.grp * kCW;
+    const unsigned int es = sizeof(T), H = (unsigned int)a.H, first = (unsigned int)p.grp * CW;
     const bool active = first + c0 < H;
     const unsigned int row_bytes = H * es, at_h = (active ? c0 * es : kOutside) + (unsigned int)t0 * row_bytes;
     const unsigned int at_u = at_h + (unsigned int)t0 * (G - 1) * row_bytes;
@@ -424,9 +430,9 @@ __global__ __launch_bounds__(64 * W, 4) void gated_backward_kernel(const GatedAr
             raw[j][g] = load_raw_at<T, VEC>(ru, at_u + (unsigned int)(j * G + g) * row_bytes);
         rawg[j] = load_raw_at<T, VEC>(rg, at_h + (unsigned int)j * row_bytes);
     }
-    const unsigned int ch = first + lane;                    // wave 0: a lane for each channel of the tile
-    const bool act = ch < H;
-    const float in0 = w == 0 && p.lt + 1 == a.n_lt && act && a.dlast ? a.dlast[(size_t)p.b * H + ch] : 0.0f;
+    const unsigned int ch = first + lane % CW;               // wave 0: a lane for each channel of the tile
+    const bool act = ch < H, one = lane < CW && act;
+    const float in0 = w == 0 && p.lt + 1 == a.n_lt && one && a.dlast ? a.dlast[(size_t)p.b * H + ch] : 0.0f;
     float before[VEC];                                       // the state in front of the tile
 #pragma unroll
     for (int k = 0; k < VEC; ++k) before[k] = active ? a.ckpt[((size_t)p.b * a.n_lt + p.lt) * H + first + c0 + k] : 0.0f;
@@ -505,15 +511,15 @@ __global__ __launch_bounds__(64 * W, 4) void gated_backward_kernel(const GatedAr
             S[k] = M[k] = 0.0f;
         }
     }
-    if (w == 0) s_in[lane] = in0;
+    if (w == 0 && lane < CW) s_in[lane] = in0;
     __syncthreads();
     const bool more = LOOK && p.lt > 0;
-    word_t *rec = a.rec + ((size_t)p.chain * a.n_lt + p.lt) * (3 * kCW);
+    word_t *rec = a.rec + ((size_t)p.chain * a.n_lt + p.lt) * (3 * CW);
     float ta = 1.0f, tm = 0.0f;
-    if (w == 0) {
+    if (w == 0 && lane < CW) {
 #pragma unroll
         for (int q = W - 1; q >= 0; --q) { tm = fmaf(s_a[q][lane], tm, s_m[q][lane]); ta *= s_a[q][lane]; }
-        if (more && act && p.lt + 1 < a.n_lt) { put(rec + lane, ta, a.tag + 1); put(rec + kCW + lane, tm, a.tag + 1); }
+        if (more && act && p.lt + 1 < a.n_lt) { put(rec + lane, ta, a.tag + 1); put(rec + CW + lane, tm, a.tag + 1); }
     }
     // the state in front of each of this thread's steps
     for (int q = 0; q < w; ++q)
@@ -545,11 +551,11 @@ __global__ __launch_bounds__(64 * W, 4) void gated_backward_kernel(const GatedAr
 #pragma unroll
         for (int k = 0; k < (int)(sizeof(v) / sizeof(v[0])); ++k) v[k] = s_in[c + k];
     };
-    if (w == 0 && act) {
+    if (w == 0 && one) {
         float in1[1];
         entering(lane, in1);
         const float out = fmaf(ta, in1[0], tm);
-        if (more) put(rec + 2 * kCW + lane, out, a.tag + 2);
+        if (more) put(rec + 2 * CW + lane, out, a.tag + 2);
         if (a.dh0 && p.lt == 0) a.dh0[(size_t)p.b * H + ch] = out;
     }
     float m[VEC];
@@ -638,23 +644,36 @@ __global__ __launch_bounds__(256) void gated_clear_kernel(ulonglong2 *p, size_t 
 // ------------------------------------------------------------------ host
 constexpr size_t kCtrl = (size_t)kQueues * kQueuePitch * sizeof(unsigned int);
 struct Shape {
-    int n_lt, groups;
+    int cw, n_lt, groups;
     long long chains, tiles;
     size_t bytes;                 // control block, and carry records where there is more than one tile along L
 };
 
+// 16 channels x 512 steps in place of 64 x 128.  Rows that leave most of a wide tile idle: forward 8 x 21715 x 16 bf16 26 -> 9 us, 64 x
+// 20000 x 16 fp32, three gates 134 -> 67, 64 x 2000 x 32 13 -> 9; with 38 channels 59 -> 76.  And sequences that one such tile
+// holds, which nobody then waits for, as long as the device holds them all at once: 4 x 469 x 464 5.9 -> 4.4, 64 x 300 x 64 6.5 ->
+// 4.6; with twice as many 8.5 -> 12.5 (8 x 400 x 1000: a row's 32 bytes come with lines of 128).  Backward alike.
+bool narrow_tiles(int B, int L, int H)
+{
+    const long long chains = (long long)B * ((H + kNarrow - 1) / kNarrow);
+    return L > tile_steps(kWide) && (H <= 32 || (L <= tile_steps(kNarrow) && chains <= 256));
+}
 bool shape_of(int dtype, int B, int L, int H, int G, Shape *s)
 {
     if ((dtype != PARARNN_F32 && dtype != PARARNN_BF16) || B < 1 || L < 1 || H < 1 || (G != 2 && G != 3)) return false;
-    s->n_lt = (int)(((long long)L + kTT - 1) / kTT);
-    s->groups = (H + kCW - 1) / kCW;
-    s->chains = (long long)B * s->groups;
-    s->tiles = s->chains * s->n_lt;
-    s->bytes = s->n_lt > 1 ? kCtrl + (size_t)s->tiles * 3 * kCW * sizeof(word_t) : 256;
+    auto cut = [&](int cw) {
+        s->cw = cw;
+        s->n_lt = (int)(((long long)L + tile_steps(cw) - 1) / tile_steps(cw));
+        s->groups = (H + cw - 1) / cw;
+        s->chains = (long long)B * s->groups;
+        s->tiles = s->chains * s->n_lt;
+    };
+    cut(narrow_tiles(B, L, H) ? kNarrow : kWide);
+    s->bytes = s->n_lt > 1 ? kCtrl + (size_t)s->tiles * 3 * s->cw * sizeof(word_t) : 256;
     return true;
 }
 
-// Row offsets of a tile are 32-bit (128 steps x 3 gates x 4 bytes x 2^20 channels), and so are the numbers of a launch's threads (512 of
+// Row offsets of a tile are 32-bit (128 steps x 3 gates x 4 bytes x 2^20 channels; 512 steps of up to 4096), and so are the numbers of a launch's threads (512 of
 // a tile; one for each channel of a walk).
 bool size_ok(const Shape &s, int B, int H)
 {
@@ -683,23 +702,25 @@ hipError_t launch_clear(void *ws, size_t bytes, hipStream_t st)
 }
 
 // LK: 0 for a single tile along L, of TT steps
-template <typename T, int G, int VEC, int LK, int TT = kTT> void launch_tiles(const GatedArgs &a, bool backward, hipStream_t st)
+template <typename T, int G, int VEC, int CW, int LK, int TT = tile_steps(CW)> void launch_tiles(const GatedArgs &a, bool backward, hipStream_t st)
 {
-    constexpr int C = TT / (kWaves * (64 * VEC / kCW));
+    constexpr int C = TT / (kWaves * (64 * VEC / CW));
     const dim3 grid((unsigned)a.chains * a.n_lt), block(64 * kWaves);
-    if (backward) hipLaunchKernelGGL((gated_backward_kernel<T, G, VEC, kWaves, C, LK>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((gated_forward_kernel<T, G, VEC, kWaves, C, LK>), grid, block, 0, st, a);
+    if (backward) hipLaunchKernelGGL((gated_backward_kernel<T, G, VEC, CW, kWaves, C, LK>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((gated_forward_kernel<T, G, VEC, CW, kWaves, C, LK>), grid, block, 0, st, a);
 }
-template <typename T, int G> hipError_t launch_tiles_of(const GatedArgs &a, bool backward, bool pairs, hipStream_t st)
+template <typename T, int G> hipError_t launch_tiles_of(const GatedArgs &a, int cw, bool backward, bool pairs, hipStream_t st)
 {
     const int look = a.n_lt == 1 ? 0 : wide_look(a) ? 4 : 1;
 #define PARARNN_GATED(VEC)                                                    \
     do {                                                                      \
-        if (look == 0 && a.L <= 32) launch_tiles<T, G, VEC, 0, 32>(a, backward, st); \
-        else if (look == 0 && a.L <= 64) launch_tiles<T, G, VEC, 0, 64>(a, backward, st); \
-        else if (look == 0) launch_tiles<T, G, VEC, 0>(a, backward, st);      \
-        else if (look == 1) launch_tiles<T, G, VEC, 1>(a, backward, st);      \
-        else launch_tiles<T, G, VEC, 4>(a, backward, st);                     \
+        if (cw == kNarrow && look == 0) launch_tiles<T, G, VEC, kNarrow, 0>(a, backward, st);        \
+        else if (cw == kNarrow) launch_tiles<T, G, VEC, kNarrow, 1>(a, backward, st);                 \
+        else if (look == 0 && a.L <= 32) launch_tiles<T, G, VEC, kWide, 0, 32>(a, backward, st);      \
+        else if (look == 0 && a.L <= 64) launch_tiles<T, G, VEC, kWide, 0, 64>(a, backward, st);      \
+        else if (look == 0) launch_tiles<T, G, VEC, kWide, 0>(a, backward, st);                       \
+        else if (look == 1) launch_tiles<T, G, VEC, kWide, 1>(a, backward, st);                       \
+        else launch_tiles<T, G, VEC, kWide, 4>(a, backward, st);                                      \
     } while (0)
     if (pairs) PARARNN_GATED(2);
     else PARARNN_GATED(1);
@@ -707,11 +728,11 @@ template <typename T, int G> hipError_t launch_tiles_of(const GatedArgs &a, bool
     return hipGetLastError();
 }
 
-int launch_of(int dtype, int G, const GatedArgs &a, bool backward, bool pairs, hipStream_t st)
+int launch_of(int dtype, int G, const GatedArgs &a, int cw, bool backward, bool pairs, hipStream_t st)
 {
     const hipError_t e = dtype == PARARNN_BF16
-                             ? (G == 2 ? launch_tiles_of<unsigned short, 2>(a, backward, pairs, st) : launch_tiles_of<unsigned short, 3>(a, backward, pairs, st))
-                             : (G == 2 ? launch_tiles_of<float, 2>(a, backward, pairs, st) : launch_tiles_of<float, 3>(a, backward, pairs, st));
+                             ? (G == 2 ? launch_tiles_of<unsigned short, 2>(a, cw, backward, pairs, st) : launch_tiles_of<unsigned short, 3>(a, cw, backward, pairs, st))
+                             : (G == 2 ? launch_tiles_of<float, 2>(a, cw, backward, pairs, st) : launch_tiles_of<float, 3>(a, cw, backward, pairs, st));
     return e == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
 }
 
@@ -733,9 +754,9 @@ bool take_workspace(void *workspace, const Shape &s, unsigned int spin_limit, Ga
     a->rec = reinterpret_cast<word_t *>(ws + kCtrl);
     a->queues = (int)std::min<long long>(kQueues, s.chains);
     a->spin_limit = spin_limit;
-    // FNV-1a; what the words are used for depends on the numbers of chains and tiles alone
+    // FNV-1a; what the words are used for depends on the tiles alone
     unsigned long long sig = 1469598103934665603ull;
-    for (unsigned long long v : {0x6761746564ull, (unsigned long long)s.n_lt, (unsigned long long)s.chains})
+    for (unsigned long long v : {0x6761746564ull, (unsigned long long)s.n_lt, (unsigned long long)s.chains, (unsigned long long)s.cw})
         for (int i = 0; i < 8; ++i) sig = (sig ^ (v >> (8 * i) & 0xff)) * 1099511628211ull;
     bool fill = true;
     a->tag = workspace_epoch(workspace, sig ? sig : 1, st, &fill);
@@ -787,7 +808,7 @@ int gated_forward(int dtype, const void *u, const float *h0, const int *lengths,
         workspace_forget(workspace);
         return PARARNN_HIP_ERROR;
     }
-    const int rc = launch_of(dtype, G, a, false, rows_of(2, H, dtype, {u, h}), st);
+    const int rc = launch_of(dtype, G, a, s.cw, false, rows_of(2, H, dtype, {u, h}), st);
     if (rc != PARARNN_OK && s.n_lt > 1) workspace_forget(workspace);
     return rc;
 }
@@ -812,7 +833,7 @@ int gated_backward(int dtype, const void *u, const float *checkpoints, const int
         workspace_forget(workspace);
         return PARARNN_HIP_ERROR;
     }
-    const int rc = launch_of(dtype, G, a, true, rows_of(2, H, dtype, {u, dL_dh, dL_du}), st);
+    const int rc = launch_of(dtype, G, a, s.cw, true, rows_of(2, H, dtype, {u, dL_dh, dL_du}), st);
     if (rc != PARARNN_OK && s.n_lt > 1) workspace_forget(workspace);
     return rc;
 }

@@ -36,6 +36,7 @@ struct Cell : torch::CustomClassHolder {
                         float *, void *, void *, size_t, void *);
     using Parts = size_t (*)(int, int, int, int, int, int, size_t *);
     int number = -1, G = 0, S = 0;
+    bool keeps_small = false;      // whether a workspace is kept for problems of any size
     std::string what;
     Ws ws_fn = nullptr, ws_fused_fn = nullptr;
     Parts parts_fn = nullptr;      // not in a library built before there was one
@@ -210,7 +211,7 @@ private:
     // Whether this call's front is one to keep (device_), and a kept one if there is one (ws_, kept_).  Returns its size.
     size_t look(const Cell &c, bool back, int code, const Dims &d, int64_t n_iters, const Tensor &like, size_t *rest)
     {
-        if ((double)d.B * d.L * d.H < kSmall) return 0;
+        if (!c.keeps_small && (double)d.B * d.L * d.H < kSmall) return 0;
         const auto cur = c10::hip::getCurrentHIPStream();
         hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
         if (cur.device_index() != like.get_device() || hipStreamIsCapturing(cur.stream(), &cap) != hipSuccess ||
@@ -481,6 +482,7 @@ const Cell &gated_cell()
         Cell *r = new Cell;
         r->what = "pararnn_gated";
         r->fwd_fn = reinterpret_cast<Cell::Fwd>(&name);      // never called: a name no other cell has
+        r->keeps_small = true;                               // whatever has records here has several tiles, and clearing is a launch of its own
         r->parts_fn = [](int dtype, int B, int L, int H, int, int, size_t *rest) {
             *rest = 0;
             return pararnn_gated_workspace_bytes(dtype, B, L, H, 2);
@@ -834,6 +836,8 @@ struct GatedLayer : torch::autograd::Function<GatedLayer> {
                                  bool train)
     {
         const On on(x, "x", {});
+        for (const OptTensor &t : {OptTensor(Wx), bias})
+            if (has(t) && t->device() != x.device()) throw py::value_error("x, Wx and bias must be on one device");
         Tensor u = project(x, Wx, bias, n_heads, {}, {}, {});
         GatedOut r = gated_solve(u, h0, lengths, train, {}, {}, {}, {});
         if (train) ctx->save_for_backward({x, Wx, u, r.ckpt, or_none(lengths), or_none(bias), or_none(h0)});

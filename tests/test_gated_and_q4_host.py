@@ -50,10 +50,10 @@ def test_gated_refusals(lib):
     fwd, bwd = lib.pararnn_gated_forward, lib.pararnn_gated_backward
     n = 1 << 30
 
-    def forward(dtype=F32, u=A, h0=A, lengths=A, B=2, L=300, H=64, G=2, h=A, last=A, ck=A, ws=A, bytes=n):
+    def forward(dtype=F32, u=A, h0=A, lengths=A, B=2, L=3000, H=64, G=2, h=A, last=A, ck=A, ws=A, bytes=n):
         return fwd(dtype, u, h0, lengths, B, L, H, G, h, last, ck, ws, bytes, None)
 
-    def backward(dtype=F32, u=A, ck=A, lengths=A, g=A, dlast=A, B=2, L=300, H=64, G=2, du=A, dh0=A, ws=A, bytes=n):
+    def backward(dtype=F32, u=A, ck=A, lengths=A, g=A, dlast=A, B=2, L=3000, H=64, G=2, du=A, dh0=A, ws=A, bytes=n):
         return bwd(dtype, u, ck, lengths, g, dlast, B, L, H, G, du, dh0, ws, bytes, None)
     for call in (forward, backward):
         for kw in (dict(dtype=2), dict(u=None), dict(B=0), dict(L=-1), dict(H=0), dict(G=1), dict(G=4), dict(ws=None), dict(ws=A + 16),
@@ -61,9 +61,9 @@ def test_gated_refusals(lib):
             assert call(**kw) == INVALID, (call, kw)
         assert call(H=(1 << 20) + 1) == UNSUPPORTED
         # more tiles, or channels of all sequences, than a launch has threads for
-        assert call(B=1 << 23, L=1, H=64, bytes=1 << 60) == UNSUPPORTED and call(B=1 << 14, L=129 << 10, H=1, bytes=1 << 60) == UNSUPPORTED
+        assert call(B=1 << 23, L=1, H=64, bytes=1 << 60) == UNSUPPORTED and call(B=1 << 14, L=129 << 13, H=1, bytes=1 << 60) == UNSUPPORTED
         assert call(B=1 << 13, L=1, H=1 << 20, bytes=1 << 60) == UNSUPPORTED
-        assert call(bytes=lib.pararnn_gated_workspace_bytes(F32, 2, 300, 64, 2) - 1) == TOO_SMALL
+        assert call(bytes=lib.pararnn_gated_workspace_bytes(F32, 2, 3000, 64, 2) - 1) == TOO_SMALL
         assert call(dtype=BF16, u=A + 1) == INVALID
     for kw in (dict(h=None), dict(h=A + 2), dict(h0=A + 2), dict(last=A + 2), dict(ck=A + 2)):
         assert forward(**kw) == INVALID, kw

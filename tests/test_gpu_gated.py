@@ -50,7 +50,7 @@ def run_and_check(P, u, h0, g, dlast, lengths=None, device=None):
 
 
 SIZES = [(1, 1, 1), (2, 1, 64), (3, 2, 7), (2, 16, 8), (2, 17, 65), (1, 127, 64), (1, 128, 72), (2, 129, 63), (1, 256, 8),
-         (2, 257, 200), (3, 300, 96), (1, 1200, 16)]
+         (2, 257, 200), (3, 300, 96), (1, 1200, 16), (3, 513, 31), (2, 512, 64), (1, 513, 65), (2, 2100, 20), (1, 1025, 33), (9, 200, 460)]
 
 
 @pytest.mark.parametrize("G", [2, 3])
@@ -441,11 +441,14 @@ def test_refusals(P):
         (ValueError, lambda: P.gated_forward(u, out=(h[:, :5], last))),
         (RuntimeError, lambda: P.gated_forward(torch.zeros(0, 10, 2, 16, device="cuda"))),
         (RuntimeError, lambda: P.gated_forward(torch.zeros(2, 0, 2, 16, device="cuda"))),
-        (RuntimeError, lambda: P.gated_forward(torch.zeros(1, 300, 2, 16, device="cuda"), workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))),
+        (RuntimeError, lambda: P.gated_forward(torch.zeros(1, 3000, 2, 16, device="cuda"), workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))),
         (ValueError, lambda: P.gated_backward(u, ckpt[:, :, :8].contiguous(), h)),
         (ValueError, lambda: P.gated_backward(u, ckpt.double(), h)),
         (ValueError, lambda: P.gated_backward(u, ckpt, h[:, :5])),
         (ValueError, lambda: P.gated_backward(u, ckpt, h, torch.zeros(2, 15, device="cuda"))),
+        (ValueError, lambda: P.gated_layer(torch.zeros(1, 3, 64, device="cuda"), torch.zeros(2, 64, 64))),
+        (ValueError, lambda: P.gated_layer(torch.zeros(1, 3, 64, device="cuda"), torch.zeros(1, 64, 64, device="cuda"))),
+        (ValueError, lambda: P.gated_layer(torch.zeros(1, 3, 64, device="cuda"), torch.zeros(2, 64, 64, device="cuda"), torch.zeros(2, 64))),
     ]
     for error, call in bad:
         with pytest.raises(error):
