@@ -467,7 +467,7 @@ int pararnn_input_projection_backward(int dtype, const void *x, const float *Wx,
  * du_f = lam (h_{l-1} - v) f (1 - f), dL_dh0 = f_1 lam_1.
  * Arithmetic in fp32; h and dL_du are rounded once.  Results are bit-reproducible.  Tensors need
  * the alignment of their elements; an even H and the alignment of two are faster.  H <= 1 048 576,
- * B * H < 2^32 and less than 2^23 tiles of 64 channels x 128 timesteps (else UNSUPPORTED).  A wait that
+ * B * H < 2^32 and less than 2^23 tiles, of 64 channels x 128 timesteps or 16 x 512 (H <= 32, some of few tiles; else UNSUPPORTED).  A wait that
  * runs out (see pararnn_set_spin_limit; it takes a broken promise for the workspace) gives NaN from there on.  Any number
  * of calls may run at once on workspaces of their own; a call captured into a graph may be replayed.
  */

@@ -26,12 +26,12 @@ def rnn_apply(cell: str, params, u, h0=None, tol: float = 1e-6, max_iter: int = 
 
 def gated_apply(u, h0=None, lengths=None):
     """(h, h_last) of the gated linear recurrence (`gated_forward`), differentiable with respect to u and h0
-    (`gated_backward`)."""
+    (`gated_backward`), once."""
     return _host.gated_apply(u, h0, lengths)
 
 
 def gated_layer(x, Wx, bias=None, h0=None, lengths=None, n_heads: int = 1):
     """The input projection followed by the gated linear recurrence, differentiable end to end (one node): x [B][L][H],
-    Wx fp32 [G][H][H / n_heads] with G = 2 or 3 gates.  Returns (h, h_last).  Rows of x behind a sequence's length take no part,
+    Wx fp32 [G][H][H / n_heads] with G = 2 or 3 gates.  Returns (h, h_last).  No second derivatives.  Rows of x behind a sequence's length take no part,
     but have to be finite when a gradient is wanted (their products with zeros are added up in dWx)."""
     return _host.gated_layer(x, Wx, bias, h0, lengths, n_heads)

@@ -8,6 +8,7 @@
 #include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/utils/pybind.h>
 #include <torch/custom_class.h>
 
@@ -119,8 +120,8 @@ struct Dims { int B, L, H; };
 // call as before.  A call takes a front out while it enqueues its work, and the next one that gets it is behind it in the
 // same stream; calls of several threads find different ones.  Bounds per device: kMost fronts and a thirty-second of its
 // memory, the least recently used go first, and all of them when torch's allocator would take more memory (GiveBack).  Under stream
-// capture, with a workspace or a stream of the caller's, for small problems (0.5 us of host time to look would show there)
-// and for kernels without records nothing is kept.
+// capture, with a workspace or a stream of the caller's, for small problems (0.5 us of host time to look would show there; not
+// those of the gated recurrence, where clearing is a launch more) and for kernels without records nothing is kept.
 using WsKey = std::array<int64_t, 8>;
 constexpr size_t kMost = 16;
 constexpr double kSmall = 1 << 20;       // timestep-channels; below, most calls take kernels without records and 10-20 us
@@ -805,6 +806,23 @@ void refuse_foreign_leaves(std::initializer_list<Tensor> inputs)
     }
 }
 
+// Gradients of a backward pass that itself is recorded (create_graph): the kernels' results have no history, so a node that says so
+// is put between them and what they depend on, and a derivative of them is an error in place of a missing term.
+void once(variable_list &out, const variable_list &inputs, const variable_list &grads)
+{
+    if (!at::GradMode::is_enabled()) return;
+    variable_list all(1);
+    for (const variable_list *from : {&inputs, &grads})
+        for (const Tensor &t : *from)
+            if (t.defined() && t.requires_grad()) all.push_back(t);
+    for (Tensor &t : out)
+        if (t.defined()) {
+            all[0] = t;
+            auto refuse = std::make_shared<torch::autograd::DelayedError>("the gated recurrence has no second derivatives", (int64_t)all.size());
+            t = (*refuse)(variable_list(all))[0];
+        }
+}
+
 // The gated linear recurrence: gated_forward with gated_backward as its gradient.
 struct Gated : torch::autograd::Function<Gated> {
     static variable_list forward(AutogradContext *ctx, Tensor u, OptTensor h0, OptTensor lengths, bool train)
@@ -825,6 +843,7 @@ struct Gated : torch::autograd::Function<Gated> {
         const bool nh = need(v[3].defined());
         GatedGrads g = gated_adjoint(v[0], v[1], dense(grads[0]), dense(grads[1]), v[2], nh, {}, {}, {});
         out[0] = g.du; out[1] = g.dh0;
+        once(out, v, grads);
         return out;
     }
     static OptTensor dense(const Tensor &g) { return g.defined() ? OptTensor(g.contiguous()) : OptTensor(); }
@@ -862,6 +881,7 @@ struct GatedLayer : torch::autograd::Function<GatedLayer> {
             if (nw) out[1] = p.dW;
             out[2] = p.db;
         }
+        once(out, v, grads);
         return out;
     }
 };

@@ -455,3 +455,56 @@ def test_refusals(P):
             call()
     with pytest.raises(RuntimeError):           # H beyond what row offsets reach
         P.gated_forward(torch.zeros(1, 1, 2, (1 << 20) + 64, device="cuda"))
+
+
+@pytest.mark.parametrize("call", ["layer", "apply"])
+def test_second_derivatives_are_refused(P, call):
+    """Gradients of a recorded backward pass have their values, and a derivative of them is an error, not a missing term."""
+    u, h0, g, _ = problem(2, 70, 64, 2, torch.float32, seed=91)
+    b = h0.cuda().requires_grad_()
+    if call == "apply":
+        a = u.cuda().requires_grad_()
+        h, _ = P.gated_apply(a, b)
+    else:
+        a = u[:, :, 0].contiguous().cuda().requires_grad_()
+        W = (torch.randn(2, 64, 64, generator=torch.Generator().manual_seed(92)) / 8).cuda()
+        h, _ = P.gated_layer(a, W, None, b)
+    want = torch.autograd.grad(h, (a, b), g.cuda(), retain_graph=True)
+    got = torch.autograd.grad(h, (a, b), g.cuda(), create_graph=True)
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+        with pytest.raises(RuntimeError, match="second derivatives"):
+            torch.autograd.grad(x.sum(), a, allow_unused=True)
+
+
+def test_threads(P):
+    """Calls of two threads on one stream and on two, kept workspaces and all."""
+    import threading
+    problems = [problem(3, 700, 96, 3, torch.bfloat16, seed=93 + k) for k in range(2)]
+    on = [(u.cuda(), h0.cuda(), g.cuda()) for u, h0, g, _ in problems]
+
+    def both(u, h0, g):
+        h, last, ckpt = P.gated_forward(u, h0, checkpoints=True)
+        return (h, last, *P.gated_backward(u, ckpt, g))
+
+    want = [both(*t) for t in on]
+    torch.cuda.synchronize()
+    for streams in ((None, None), (torch.cuda.Stream(), torch.cuda.Stream())):
+        got = [[], []]
+
+        def work(k):
+            with torch.cuda.stream(streams[k]):
+                for _ in range(20):
+                    got[k].append(both(*on[k]))
+
+        threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        torch.cuda.synchronize()
+        for k in range(2):
+            assert len(got[k]) == 20
+            for r in got[k]:
+                for x, y in zip(r, want[k]):
+                    assert torch.equal(x, y)
