@@ -39,18 +39,25 @@ __device__ __forceinline__ unsigned int pack8(const int (&q)[8])
 }
 __device__ __forceinline__ int code_at(unsigned int w, int e) { return (int)(w >> (4 * (e >> 1) + 16 * (e & 1)) & 15u) - 8; }
 
-// the eight numbers 24 + q of a word, as the matrix cores take them
-__device__ __forceinline__ bf8v operand(unsigned int w)
+// 16.0 twice, in a vector register: an instruction takes one scalar, and the mask is one
+__device__ __forceinline__ unsigned int sixteens()
 {
-    constexpr unsigned int mask = 0x00780078u, one = 0x41804180u;        // the mantissa bits above 1/8, and 16.0 twice
+    unsigned int x = 0x41804180u;
+    asm("" : "+v"(x));
+    return x;
+}
+// the eight numbers 24 + q of a word, as the matrix cores take them
+__device__ __forceinline__ bf8v operand(unsigned int w, unsigned int one)
+{
+    constexpr unsigned int mask = 0x00780078u;                           // the mantissa bits above 1/8
     const u4v r = {((w << 3) & mask) | one, ((w >> 1) & mask) | one, ((w >> 5) & mask) | one, ((w >> 9) & mask) | one};
     return __builtin_bit_cast(bf8v, r);
 }
 
 // the same less 24, exact too: for fp32, where the 24 and its product would cost the sums three bits
-__device__ __forceinline__ bf8v operand_signed(unsigned int w)
+__device__ __forceinline__ bf8v operand_signed(unsigned int w, unsigned int one)
 {
-    const u4v r = __builtin_bit_cast(u4v, operand(w));
+    const u4v r = __builtin_bit_cast(u4v, operand(w, one));
     u4v q;
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
@@ -257,6 +264,7 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
 
     const u4v minus24 = {0xc1c0c1c0u, 0xc1c0c1c0u, 0xc1c0c1c0u, 0xc1c0c1c0u};
     const bf8v offset = __builtin_bit_cast(bf8v, minus24);
+    const unsigned int one = sixteens();
     f4v total[NT][MT];
 #pragma unroll
     for (int g = 0; g < NT; ++g)
@@ -305,7 +313,7 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
             for (int g = 0; g < NT; ++g) {
                 bf8v b[STEPS];
 #pragma unroll
-                for (int s = 0; s < STEPS; ++s) b[s] = TERMS == 1 ? operand(q[g][p * STEPS + s]) : operand_signed(q[g][p * STEPS + s]);
+                for (int s = 0; s < STEPS; ++s) b[s] = TERMS == 1 ? operand(q[g][p * STEPS + s], one) : operand_signed(q[g][p * STEPS + s], one);
                 const float scale = __uint_as_float(sc[g][G32 ? p : 0] << 16);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
@@ -461,19 +469,183 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
     }
 }
 
+// ------------------------------------------------------------------ products of many rows
+// A workgroup: 128 rows x 64 NW channels of a gate, 2 x NW waves of 64 x 64 each that go through the inputs together, a unit at a time.  Rows come
+// into LDS once for all of them (fp32: as their three terms), two places in turn with one barrier a unit; weights go from
+// memory into the operand registers as above, the next unit's on their way meanwhile.
+template <typename T, int NW, int KS, bool G32>
+__global__ __launch_bounds__(128 * NW * KS, 2) void q4_tiles_kernel(const RowsQ4Args a)
+{
+    constexpr int TERMS = Eight<T>::TERMS, M = 128, MT = 4, NT = 4, THREADS = 128 * NW;
+    constexpr int LOADS = M * 8 / THREADS;                    // eights of x that a thread brings
+    __shared__ u4v s_x[KS][2][TERMS][M * 8];
+    const int lane = threadIdx.x & 63, n = lane & 15, kq = lane >> 4, all_w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int part = KS == 1 ? 0 : all_w / (2 * NW), w = KS == 1 ? all_w : all_w % (2 * NW);
+    // the tiles of 64 channels of all gates that have a head's inputs, NW at a time
+    const unsigned int in_head = (unsigned)a.dh / 64, all = in_head * a.G, across = (all + NW - 1) / NW, per_rows = across * (a.tiles / 4 / in_head);
+    const unsigned int mb = blockIdx.x / per_rows, rest = blockIdx.x - mb * per_rows, head = rest / across;
+    unsigned int tile = (rest - head * across) * NW + w / 2;
+    const bool mine = tile < all;                             // (a wave behind the last tile multiplies that one again and writes nothing)
+    tile = mine ? tile : all - 1;
+    const int gate = (int)(tile / in_head), ct = (int)(head * in_head + tile - gate * in_head) * 4, wm = (w & 1) * 64;
+    const int m0 = (int)mb * M;
+    const T *x = static_cast<const T *>(a.x) + (size_t)m0 * a.H + (size_t)head * a.dh;
+    // loads by resources: what all lanes share is in scalar registers, and nothing is added up for a load
+    auto resource = [](const void *p, size_t bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (unsigned int)bytes, 0x27000); };
+    const unsigned int esH = a.H * (unsigned int)sizeof(T);
+    const buf_rsrc rx = resource(x, (size_t)(a.rows - m0 < M ? a.rows - m0 : M) * esH - (size_t)head * a.dh * sizeof(T));
+    const size_t tile0 = (size_t)gate * a.tiles + ct;
+    const buf_rsrc rw = resource(a.packed + tile0 * a.nu * 64, (size_t)NT * a.nu * 512);
+    const buf_rsrc rs = resource(a.scales + tile0 * a.ng * 16, (size_t)NT * a.ng * 32);
+
+    unsigned int from[LOADS], to[LOADS];                      // bytes, places
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+        const int id = j * THREADS + threadIdx.x % THREADS, r = id / 8, c = id % 8;
+        from[j] = ((unsigned int)(m0 + r < a.rows ? r : 0) * a.H + c * 8) * sizeof(T);
+        to[j] = r * 8 + (c ^ (r & 7));
+    }
+    Eight<T> raw[LOADS];
+    u2v q[NT];
+    unsigned int sc[NT][2];
+    const int last = a.nu - 1;                                // (behind it, it is read again: a load without a branch has no wait of its own)
+    auto load_x = [&](int ku) {
+        const unsigned int k = (unsigned)(ku < last ? ku : last) * 64 * (unsigned)sizeof(T);
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j)
+#pragma unroll
+            for (int h = 0; h < Eight<T>::CHUNKS; ++h) raw[j].c[h] = __builtin_amdgcn_raw_buffer_load_b128(rx, from[j] + 16 * h, k, 0);
+    };
+    auto store_x = [&](int buf) {
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            bf8v t[TERMS];
+            raw[j].terms(t);
+#pragma unroll
+            for (int e = 0; e < TERMS; ++e) s_x[part][buf][e][to[j]] = __builtin_bit_cast(u4v, t[e]);
+        }
+    };
+    auto load_weights = [&](int ku) {
+        ku = ku < last ? ku : last;
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            q[c] = __builtin_amdgcn_raw_buffer_load_b64(rw, lane * 8, (unsigned)(c * a.nu + ku) * 512, 0);
+            const unsigned int group = c * a.ng + (G32 ? 2 * ku : ku >> a.unit_shift);
+            sc[c][0] = __builtin_amdgcn_raw_buffer_load_b16(rs, n * 2, group * 32, 0);
+            if constexpr (G32) sc[c][1] = __builtin_amdgcn_raw_buffer_load_b16(rs, n * 2, group * 32 + 32, 0);
+        }
+    };
+    float bias[NT];
+#pragma unroll
+    for (int c = 0; c < NT; ++c) bias[c] = a.bias ? a.bias[(size_t)gate * a.H + (ct + c) * 16 + n] : 0.0f;
+    const u4v minus24 = {0xc1c0c1c0u, 0xc1c0c1c0u, 0xc1c0c1c0u, 0xc1c0c1c0u};
+    const bf8v offset = __builtin_bit_cast(bf8v, minus24);
+    const unsigned int one = sixteens();
+    f4v total[NT][MT];
+#pragma unroll
+    for (int c = 0; c < NT; ++c)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) total[c][m] = f4v{0, 0, 0, 0};
+
+    load_x(part);
+    load_weights(part);
+    store_x(0);
+    load_x(part + KS);
+    for (int i = 0, ku = part; i * KS < a.nu; ++i, ku += KS) {
+        __syncthreads();               // this unit's x is there, and nobody reads the other place any more
+        store_x(~i & 1);
+        load_x(ku + 2 * KS);
+        bf8v b[NT][2];
+        float scale[NT][2];
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) b[c][s] = TERMS == 1 ? operand(q[c][s], one) : operand_signed(q[c][s], one);
+            scale[c][0] = __uint_as_float(sc[c][0] << 16);
+            if constexpr (G32) scale[c][1] = __uint_as_float(sc[c][1] << 16);
+        }
+        load_weights(ku + KS);
+        if (KS > 1 && ku >= a.nu) break;      // (the last round, and the barriers are behind)
+        const u4v(*const xs)[M * 8] = s_x[part][i & 1];
+        constexpr int PARTS = G32 || TERMS == 3 ? 2 : 1, STEPS = 2 / PARTS;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) {
+                bf8v t[STEPS][TERMS];
+                f4v start = {0, 0, 0, 0};
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) {
+#pragma unroll
+                    for (int e = 0; e < TERMS; ++e)
+                        t[s][e] = __builtin_bit_cast(bf8v, xs[e][(wm + 16 * m + n) * 8 + ((4 * (p * STEPS + s) + kq) ^ (n & 7))]);
+                    if constexpr (TERMS == 1) start = __builtin_amdgcn_mfma_f32_16x16x32_bf16(t[s][0], offset, start, 0, 0, 0);
+                }
+                f4v acc[NT];
+#pragma unroll
+                for (int c = 0; c < NT; ++c) acc[c] = start;
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                    for (int e = TERMS - 1; e >= 0; --e)
+#pragma unroll
+                        for (int c = 0; c < NT; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(t[s][e], b[c][p * STEPS + s], acc[c], 0, 0, 0);
+#pragma unroll
+                for (int c = 0; c < NT; ++c) total[c][m] += scale[c][G32 ? p : 0] * acc[c];
+                if constexpr (G32 && TERMS == 1 && KS == 1) __builtin_amdgcn_sched_barrier(0);
+            }
+    }
+    if constexpr (KS == 2) {
+        // one sum of both halves, where x was
+        f4v *const sums = reinterpret_cast<f4v *>(s_x) + w * (NT * MT * 64) + lane;
+        static_assert(sizeof(s_x) >= 2 * NW * NT * MT * 64 * sizeof(f4v), "");
+        __syncthreads();
+        if (part == 1)
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+#pragma unroll
+                for (int m = 0; m < MT; ++m) sums[(c * MT + m) * 64] = total[c][m];
+        __syncthreads();
+        if (part == 1) return;
+#pragma unroll
+        for (int c = 0; c < NT; ++c)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) total[c][m] += sums[(c * MT + m) * 64];
+    }
+    if (!mine) return;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int row = m0 + wm + 16 * m + 4 * kq + e;
+            if (row >= a.rows) continue;
+            const size_t at = ((size_t)row * a.G + gate) * a.H + ct * 16 + n;
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+                const float u = total[c][m][e] + bias[c];
+                if constexpr (sizeof(T) == 4) static_cast<float *>(a.out)[at + c * 16] = u;
+                else static_cast<unsigned short *>(a.out)[at + c * 16] = f32_to_bf16(u);
+            }
+        }
+}
+
 // ------------------------------------------------------------------ host
-// Rows up to which bf16 inputs take q4_rows_kernel; beyond, the weights are written out in bf16 for the tiles of the projection.  The
-// former's rate grows with the inputs of a head (its workgroups' starts and sums): 0.13 PFLOP/s for 256 of them, 0.2 for 512, 0.28
-// for 1024, 0.36 for 2048; the latter takes 9 us and 0.022 for each input of a head longer to start with, whatever the rows, and
-// then does up to 1.  (H x gates, dh): rows at which both took the same, from 128 to 4096 rows measured, and the time: (2048 x 2, 2048)
-// 1280, 57 us; (4096 x 3, 1024) 400, 42; (8192 x 2, 1024) 350, 45; (2048 x 3, 1024) 720, 38; (512 x 4, 512) 1750, 23; (1536 x 2, 384)
-// 1200, 21; (1024 x 3, 256) 1100, 18; (512 x 2, 256), (256 x 3, 64) and (64 x 2, 64) beyond 4096.  At 128 rows: 8 us to 56, 17 to 41,
-// 17 to 44, 9 to 33, 4 to 19, 6 to 17, 5 to 15, 3 to 14.
+// Rows up to which bf16 inputs are multiplied with the codes themselves; beyond, the weights are written out in bf16 for the tiles of the
+// projection, whose rate is higher by a third but which start with that.  In units of what 256 of the projection's tiles (256 x 256) take:
+// those take 8 us and, for every 256 tiles begun, 10 us and 1.4 for each 64 inputs of a head (2048 x 2 x 2048: 56 us for 65 rows,
+// 61 for 2048 and 73 for 4096; 4096 x 3 x 1024: 41 to 45 up to 1024 rows, 73 for 2048, 108 for 4096); q4_tiles_kernel takes 2 us and 4 + 2.64
+// for each 64 inputs, in proportion to the rows (46 and 88 us; 39, 74 and 144).  The projection takes over where it is ahead for a
+// fifth of such a round at least, and never for heads of up to 320 inputs.  Rows at which both took the same: 2048 x 2 x 2048 3000,
+// 4096 x 3 x 1024 2000, 2048 x 3 x 1024 3700, 2816 x 4 x 704 2700, 1024 x 3 x 256, 512 x 4 x 512 and 512 x 2 x 64 beyond 4096.
 int exact_rows(int H, int G, int n_heads)
 {
-    const double dh = H / n_heads, rate = 0.48 * dh / (dh + 700.0);
-    const double rows = (9.0 + 0.022 * dh) * 1e9 / (2.0 * G * H * dh * (1.0 / rate - 0.3));
-    return rows < 64.0 ? 64 : rows > 1e6 ? 1000000 : (int)rows;
+    const double nu = H / n_heads / 64, round = 10.0 + 1.41 * nu, own = 4.0 + 2.64 * nu;
+    if (nu <= 5.0) return 1000000000;
+    for (int r = 1; r < 64; ++r) {
+        const double rounds = (6.0 + r * round) / own;
+        if (rounds < r - 0.2) return std::max(64, (int)std::min(1e9, rounds * (1 << 24) / ((double)G * H)));
+    }
+    return 1000000000;
 }
 bool weights_ok(int H, int G, int n_heads) { return H >= 1 && G >= 1 && G <= 8 && n_heads >= 1 && H % n_heads == 0; }
 bool group_ok(int group) { return group == 32 || group == 64 || group == 128; }
@@ -518,6 +690,38 @@ constexpr int kWorkgroups = 192;        // fewer leave too much of the device id
 // for 16 against 11.8 and 12.0; a step with 2 x 8192 x 1024 5.7 and 6.9 against 5.6 and 5.7, with 2 x 4096 x 4096 7.3 and 9.3 against
 // 8.5 and 8.6; with too few workgroups, 3 x 2048 x 1024, 3.4 and 4.4 against 5.4 and 5.5.  fp32, whose terms cost more than the
 // weights: 21 and 27 against 24 and 24, 5.0 and 6.6 against 8.8 and 8.9.
+// Whether tiles of 128 rows beat the kernel of few rows.  They use a weight for twice the rows or more and need no sums of eight waves, but have
+// fewer workgroups, which take a unit in 0.7 us (fp32 3.1): it pays from a number of the latter's workgroups (64 rows x 64 channels,
+// fp32 32 x 64) on.  Both level, bf16, units of a head: that number: 1: 90, 4: 340, 8: 300, 11: 340, 16: 390, 32: 580; 4096 rows: 9.9 to
+// 5.6 us, 32 to 18, 45 to 18, 245 to 97, 155 to 70, 146 to 88.  fp32: 6: 1000, 16: 1800 (512 rows 33 to 24, 94 to 54; 4096 rows 248 to 76, 730 to
+// 319), and not with too few of either (512 x 2 x 256: 2048 rows 12.2 to 16.9, 4096 22 to 18).
+bool tiles_better(const RowsQ4Args &a, bool bf16)
+{
+    if (a.rows <= 64) return false;
+    const double groups = (double)(a.H / 64) * a.G * ((a.rows + (bf16 ? 63 : 31)) / (bf16 ? 64 : 32));
+    if (bf16) return groups > std::min(90.0 * a.nu, 300.0 + 8.0 * a.nu);
+    return groups > std::max(1100.0, 256.0 * (1.0 + 3.1 * a.nu) / (2.3 + 0.33 * a.nu));
+}
+template <typename T, int NW, int KS> hipError_t launch_tiles(const RowsQ4Args &a, long long blocks, int group, hipStream_t st)
+{
+    if (blocks * 512 >= (1ll << 32)) return hipErrorInvalidConfiguration;      // threads of a launch are numbered in 32 bits
+    const dim3 grid((unsigned)blocks), block(128 * NW * KS);
+    if (group == 32) hipLaunchKernelGGL((q4_tiles_kernel<T, NW, KS, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((q4_tiles_kernel<T, NW, KS, false>), grid, block, 0, st, a);
+    return hipGetLastError();
+}
+// bf16: 128 channels (4096 x 3 x 1024 weights, 686 rows: 36.9 us, 256 channels 45.2; 4096 rows level); where there is not one workgroup for each
+// compute unit, twice the waves share the inputs (2048 x 2 x 2048, 686 rows: 30.2 to 24.6; with two for each 46 to 51).  fp32: 256 channels,
+// for the terms of x are formed once for all of them (4096 x 3 x 1024, 4096 rows: 498 to 310 us).
+template <typename T> hipError_t launch_tiles(const RowsQ4Args &a, int group, hipStream_t st)
+{
+    constexpr int NW = sizeof(T) == 2 ? 2 : 4;
+    const int all = a.G * (a.dh / 64);                        // of a head
+    const long long blocks = (long long)(a.H / a.dh) * ((all + NW - 1) / NW) * ((a.rows + 127) / 128);
+    if constexpr (sizeof(T) == 2)
+        if (blocks <= 256 && a.nu >= 8) return launch_tiles<T, NW, 2>(a, blocks, group, st);
+    return launch_tiles<T, NW, 1>(a, blocks, group, st);
+}
 template <typename T, int NG, bool STEP> hipError_t launch_rows_of(RowsQ4Args a, int n_heads, int group, hipStream_t st)
 {
     a.dh = a.H / n_heads; a.nu = a.dh / 64; a.ng = a.dh / group; a.tiles = (unsigned)a.H / 16;
@@ -527,6 +731,8 @@ template <typename T, int NG, bool STEP> hipError_t launch_rows_of(RowsQ4Args a,
     constexpr int C4 = STEP ? 1 : 4;
     constexpr bool bf16 = sizeof(T) == 2;
     // (three terms of fp32 leave no registers for 64 rows: 46 -> 88 us for 64 of 3 x 4096 x 4096)
+    if constexpr (!STEP)
+        if (tiles_better(a, bf16)) return launch_tiles<T>(a, group, st);
     if constexpr (bf16)
         if (a.rows > 32 && enough(4, C4)) return launch_rows<T, 4, NG, C4, STEP>(a, group, st);
     if (a.rows > (bf16 ? 8 : 16) && enough(2, C4)) return launch_rows<T, 2, NG, C4, STEP>(a, group, st);

@@ -79,9 +79,9 @@ def test_q4_sizes(lib):
     for group in (0, 16, 48, 128):
         assert lib.pararnn_q4_scale_bytes(64, 1, 1, group) == 0
     ws = lib.pararnn_q4_workspace_bytes
-    few = lib.pararnn_q4_exact_rows(256, 2, 1)
-    assert few >= 1
-    assert ws(BF16, 1, few, 256, 2, 1, 64) >= 256 and ws(BF16, few + 1, 1, 256, 2, 1, 64) >= 2 * 256 * 256 * 2
+    few = lib.pararnn_q4_exact_rows(4096, 3, 1)
+    assert 64 <= few < 4000 and lib.pararnn_q4_exact_rows(128, 2, 1) >= 64
+    assert ws(BF16, 1, few, 4096, 3, 1, 64) == 256 and ws(BF16, few + 1, 1, 4096, 3, 1, 64) >= 3 * 4096 * 4096 * 2
     assert ws(F32, 1, few + 1, 256, 2, 1, 64) >= 256
     assert ws(2, 1, 1, 256, 2, 1, 64) == 0 and ws(BF16, 0, 1, 256, 2, 1, 64) == 0 and ws(BF16, 1, 1, 256, 2, 1, 48) == 0
 
@@ -114,8 +114,8 @@ def test_q4_refusals(lib):
         for kw in (dict(dtype=2), dict(x=None), dict(x=A + 8), dict(bias=A + 2), dict(B=0)):
             assert call(**kw) == INVALID, (call, kw)
     assert project(L=0) == INVALID and project(u=A + 2) == INVALID and project(u=None) == INVALID and project(ws=A + 8) == INVALID
-    many = lib.pararnn_q4_exact_rows(128, 2, 1) + 1
-    assert project(dtype=BF16, B=1, L=many, bytes=256) == TOO_SMALL and project(dtype=BF16, B=1, L=many, u=A + 2) == UNSUPPORTED
+    many = dict(dtype=BF16, B=1, L=lib.pararnn_q4_exact_rows(4096, 3, 1) + 1, H=4096, G=3)
+    assert project(bytes=256, **many) == TOO_SMALL and project(u=A + 2, **many) == UNSUPPORTED
     assert step(G=1) == INVALID and step(G=4) == INVALID and step(y=None) == INVALID and step(nxt=None) == INVALID
     assert project(B=1 << 10, L=1 << 19, H=1 << 14, heads=1 << 8) == UNSUPPORTED        # more workgroups than a launch has
     assert step(h=A + 2) == INVALID and step(nxt=A + 2) == INVALID and step(B=(1 << 20) + 1) == UNSUPPORTED

@@ -104,7 +104,7 @@ def test_products(P, rows, G, heads, dh, group, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("G,heads,dh,group", [(2, 1, 1024, 128), (4, 3, 576, 32), (3, 2, 1024, 64)])
+@pytest.mark.parametrize("G,heads,dh,group", [(8, 1, 2048, 128), (3, 1, 4096, 32), (8, 3, 704, 64)])
 @pytest.mark.parametrize("beyond", [0, 1, 300])
 def test_products_of_many_rows(P, beyond, G, heads, dh, group, dtype):
     """At the border between the two ways for bf16, and behind it."""
@@ -119,6 +119,39 @@ def test_products_of_many_rows(P, beyond, G, heads, dh, group, dtype):
     V = ref.values(codes, scales)
     err = bound(x, V, scales, heads, rounded_weights=dtype == torch.bfloat16 and beyond > 0) + 4 * ref.EPS * bias.double().abs()
     ref.check(u.view(rows, G, -1), ref.project(x, V, bias, heads), err, "u")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,G,heads,dh,group", [(2100, 4, 3, 64, 64), (2049, 4, 3, 64, 32), (900, 4, 3, 192, 64), (900, 3, 5, 192, 32),
+                                                   (1700, 3, 1, 576, 32), (1700, 3, 1, 640, 64), (1153, 8, 1, 512, 128), (1153, 8, 1, 512, 32)])
+def test_products_in_tiles(P, rows, G, heads, dh, group, dtype):
+    """Rows and channels that end inside a tile, one unit of inputs and odd numbers of them, sums of one wave and of two."""
+    codes, scales = ref.quantise(weights(G, heads, dh, seed=rows), group)
+    x = torch.randn(rows, heads * dh, generator=torch.Generator().manual_seed(rows)).to(dtype)
+    bias = torch.randn(G, heads * dh, generator=torch.Generator().manual_seed(dh))
+    Wq = P.pack_projection(codes.cuda(), scales.cuda(), n_heads=heads)
+    flat = torch.full((rows * G * heads * dh + 2,), 5.0, dtype=dtype, device="cuda")
+    u = P.input_projection_q4(x.view(1, rows, -1).cuda(), Wq, bias.cuda(), out=flat[1:-1].view(1, rows, G, heads * dh))
+    V = ref.values(codes, scales)
+    ref.check(u.view(rows, G, -1), ref.project(x, V, bias, heads), bound(x, V, scales, heads) + 4 * ref.EPS * bias.double().abs(), "u")
+    assert flat[0] == 5 and flat[-1] == 5
+    again = P.input_projection_q4(x.view(1, rows, -1).cuda(), Wq, bias.cuda())
+    assert torch.equal(u, again)
+
+
+def test_a_row_keeps_to_itself(P):
+    """A NaN in one row, an infinity in another, both in one head: those rows of that head alone, in tiles as in single rows."""
+    Wq = P.quantize_projection(weights(4, 3, 64, seed=9).cuda(), n_heads=3)
+    for rows in (3, 2100):
+        for dtype in (torch.float32, torch.bfloat16):
+            x = torch.randn(rows, 192, generator=torch.Generator().manual_seed(rows)).to(dtype).cuda()
+            want = P.input_projection_q4(x[None], Wq)[0]
+            x[1, 70], x[rows - 1, 3] = float("nan"), float("inf")
+            u = P.input_projection_q4(x[None], Wq)[0]
+            hit = torch.zeros(rows, 1, 192, dtype=torch.bool, device="cuda")
+            hit[1, :, 64:128] = hit[rows - 1, :, :64] = True
+            hit = hit.expand_as(u)
+            assert not u[hit].isfinite().any() and torch.equal(u[~hit], want[~hit])
 
 
 def test_one_row_of_another_batch_is_the_same(P):
@@ -275,7 +308,8 @@ def test_refusals(P):
         (ValueError, lambda: P.input_projection_q4(x, Wq, torch.zeros(3, 256, device="cuda"))),
         (KeyError, lambda: P.input_projection_q4(x.half(), Wq)),
         (RuntimeError, lambda: P.input_projection_q4(x[:0], Wq)),
-        (RuntimeError, lambda: P.input_projection_q4(torch.zeros(1, P.q4_exact_rows(256, 2, 2) + 1, 256, device="cuda", dtype=torch.bfloat16), Wq,
+        (RuntimeError, lambda: P.input_projection_q4(torch.zeros(1, P.q4_exact_rows(2048, 8, 1) + 1, 2048, device="cuda", dtype=torch.bfloat16),
+                                                     P.quantize_projection(torch.zeros(8, 2048, 2048, device="cuda")),
                                                      workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))),
         (ValueError, lambda: P.gated_layer_step(x, Wq)),
         (ValueError, lambda: P.gated_layer_step(row, Wq, row.bfloat16())),
