@@ -473,21 +473,21 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
 // A workgroup: 128 rows x 64 NW channels of a gate, 2 x NW waves of 64 x 64 each that go through the inputs together, a unit at a time.  Rows come
 // into LDS once for all of them (fp32: as their three terms), two places in turn with one barrier a unit; weights go from
 // memory into the operand registers as above, the next unit's on their way meanwhile.
-template <typename T, int NW, int KS, bool G32>
-__global__ __launch_bounds__(128 * NW * KS, 2) void q4_tiles_kernel(const RowsQ4Args a)
+template <typename T, int MT, int NW, int KS, bool G32>
+__global__ __launch_bounds__(64 * 8 / MT * NW * KS, 2) void q4_tiles_kernel(const RowsQ4Args a)
 {
-    constexpr int TERMS = Eight<T>::TERMS, M = 128, MT = 4, NT = 4, THREADS = 128 * NW;
+    constexpr int TERMS = Eight<T>::TERMS, M = 128, NT = 4, WM = 8 / MT, THREADS = 64 * WM * NW;
     constexpr int LOADS = M * 8 / THREADS;                    // eights of x that a thread brings
     __shared__ u4v s_x[KS][2][TERMS][M * 8];
     const int lane = threadIdx.x & 63, n = lane & 15, kq = lane >> 4, all_w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int part = KS == 1 ? 0 : all_w / (2 * NW), w = KS == 1 ? all_w : all_w % (2 * NW);
+    const int part = KS == 1 ? 0 : all_w / (WM * NW), w = KS == 1 ? all_w : all_w % (WM * NW);
     // the tiles of 64 channels of all gates that have a head's inputs, NW at a time
     const unsigned int in_head = (unsigned)a.dh / 64, all = in_head * a.G, across = (all + NW - 1) / NW, per_rows = across * (a.tiles / 4 / in_head);
     const unsigned int mb = blockIdx.x / per_rows, rest = blockIdx.x - mb * per_rows, head = rest / across;
-    unsigned int tile = (rest - head * across) * NW + w / 2;
+    unsigned int tile = (rest - head * across) * NW + w / WM;
     const bool mine = tile < all;                             // (a wave behind the last tile multiplies that one again and writes nothing)
     tile = mine ? tile : all - 1;
-    const int gate = (int)(tile / in_head), ct = (int)(head * in_head + tile - gate * in_head) * 4, wm = (w & 1) * 64;
+    const int gate = (int)(tile / in_head), ct = (int)(head * in_head + tile - gate * in_head) * 4, wm = w % WM * 16 * MT;
     const int m0 = (int)mb * M;
     const T *x = static_cast<const T *>(a.x) + (size_t)m0 * a.H + (size_t)head * a.dh;
     // loads by resources: what all lanes share is in scalar registers, and nothing is added up for a load
@@ -598,7 +598,7 @@ __global__ __launch_bounds__(128 * NW * KS, 2) void q4_tiles_kernel(const RowsQ4
     if constexpr (KS == 2) {
         // one sum of both halves, where x was
         f4v *const sums = reinterpret_cast<f4v *>(s_x) + w * (NT * MT * 64) + lane;
-        static_assert(sizeof(s_x) >= 2 * NW * NT * MT * 64 * sizeof(f4v), "");
+        static_assert(sizeof(s_x) >= WM * NW * NT * MT * 64 * sizeof(f4v), "");
         __syncthreads();
         if (part == 1)
 #pragma unroll
@@ -631,19 +631,17 @@ __global__ __launch_bounds__(128 * NW * KS, 2) void q4_tiles_kernel(const RowsQ4
 
 // ------------------------------------------------------------------ host
 // Rows up to which bf16 inputs are multiplied with the codes themselves; beyond, the weights are written out in bf16 for the tiles of the
-// projection, whose rate is higher by a third but which start with that.  In units of what 256 of the projection's tiles (256 x 256) take:
-// those take 8 us and, for every 256 tiles begun, 10 us and 1.4 for each 64 inputs of a head (2048 x 2 x 2048: 56 us for 65 rows,
-// 61 for 2048 and 73 for 4096; 4096 x 3 x 1024: 41 to 45 up to 1024 rows, 73 for 2048, 108 for 4096); q4_tiles_kernel takes 2 us and 4 + 2.64
-// for each 64 inputs, in proportion to the rows (46 and 88 us; 39, 74 and 144).  The projection takes over where it is ahead for a
-// fifth of such a round at least, and never for heads of up to 320 inputs.  Rows at which both took the same: 2048 x 2 x 2048 3000,
-// 4096 x 3 x 1024 2000, 2048 x 3 x 1024 3700, 2816 x 4 x 704 2700, 1024 x 3 x 256, 512 x 4 x 512 and 512 x 2 x 64 beyond 4096.
+// projection, whose rate is higher but which start with that.  In units of what 256 of the projection's tiles (256 x 256) take: those
+// take 8 us and, for every 256 tiles begun, 10 us and 1.4 for each 64 inputs of a head (2048 x 2 x 2048: 56 us for 65 rows, 61 for 2048,
+// 72 for 4096, 116 for 6000; 4096 x 3 x 1024: 41 to 45 up to 1024 rows, 73 for 2048, 106 for 4096); q4_tiles_kernel takes 2 us and 5 + 2.15 for
+// each 64 inputs, in proportion to the rows (46 us for 2048, 76 for 4096, 113 for 6000; 38, 64 and 120), with groups of 32 a fifth
+// more.  The projection takes over where it is ahead for a seventh of such a round at least, and never for heads of few inputs.
 int exact_rows(int H, int G, int n_heads)
 {
-    const double nu = H / n_heads / 64, round = 10.0 + 1.41 * nu, own = 4.0 + 2.64 * nu;
-    if (nu <= 5.0) return 1000000000;
+    const double nu = H / n_heads / 64, round = 10.0 + 1.41 * nu, own = 5.0 + 2.15 * nu;
     for (int r = 1; r < 64; ++r) {
         const double rounds = (6.0 + r * round) / own;
-        if (rounds < r - 0.2) return std::max(64, (int)std::min(1e9, rounds * (1 << 24) / ((double)G * H)));
+        if (rounds < r - 0.15) return std::max(64, (int)std::min(1e9, rounds * (1 << 24) / ((double)G * H)));
     }
     return 1000000000;
 }
@@ -702,25 +700,31 @@ bool tiles_better(const RowsQ4Args &a, bool bf16)
     if (bf16) return groups > std::min(90.0 * a.nu, 300.0 + 8.0 * a.nu);
     return groups > std::max(1100.0, 256.0 * (1.0 + 3.1 * a.nu) / (2.3 + 0.33 * a.nu));
 }
-template <typename T, int NW, int KS> hipError_t launch_tiles(const RowsQ4Args &a, long long blocks, int group, hipStream_t st)
+template <typename T, int MT, int NW, int KS> hipError_t launch_tiles(const RowsQ4Args &a, long long blocks, int group, hipStream_t st)
 {
     if (blocks * 512 >= (1ll << 32)) return hipErrorInvalidConfiguration;      // threads of a launch are numbered in 32 bits
-    const dim3 grid((unsigned)blocks), block(128 * NW * KS);
-    if (group == 32) hipLaunchKernelGGL((q4_tiles_kernel<T, NW, KS, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((q4_tiles_kernel<T, NW, KS, false>), grid, block, 0, st, a);
+    const dim3 grid((unsigned)blocks), block(64 * 8 / MT * NW * KS);
+    if (group == 32) hipLaunchKernelGGL((q4_tiles_kernel<T, MT, NW, KS, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((q4_tiles_kernel<T, MT, NW, KS, false>), grid, block, 0, st, a);
     return hipGetLastError();
 }
-// bf16: 128 channels (4096 x 3 x 1024 weights, 686 rows: 36.9 us, 256 channels 45.2; 4096 rows level); where there is not one workgroup for each
-// compute unit, twice the waves share the inputs (2048 x 2 x 2048, 686 rows: 30.2 to 24.6; with two for each 46 to 51).  fp32: 256 channels,
-// for the terms of x are formed once for all of them (4096 x 3 x 1024, 4096 rows: 498 to 310 us).
+// bf16: 128 channels in four waves, 64 rows x 64 channels each.  Where there is not one such workgroup for each compute unit, twice the waves share
+// the inputs (2048 x 2 x 2048, 686 rows: 30.2 to 24.6 us; with two for each 46 to 51).  Where there is one of 256 channels for each, and a head's
+// channels fill them, waves of 128 rows x 64 channels, which unpack a weight once for all of them (4096 rows: 4096 x 3 x 1024 142 to 120, 2816
+// x 4 x 704 97 to 83; 264 and 288 workgroups 28.0 to 26.2, 37.1 to 35.1, 192 23.6 to 25.5; groups of 32 with 256 18.6 to 23.8).
+// fp32: 256 channels in eight waves, for the terms of x are formed once for all of them (4096 x 3 x 1024, 4096 rows: 498 to 310).
 template <typename T> hipError_t launch_tiles(const RowsQ4Args &a, int group, hipStream_t st)
 {
-    constexpr int NW = sizeof(T) == 2 ? 2 : 4;
     const int all = a.G * (a.dh / 64);                        // of a head
-    const long long blocks = (long long)(a.H / a.dh) * ((all + NW - 1) / NW) * ((a.rows + 127) / 128);
-    if constexpr (sizeof(T) == 2)
-        if (blocks <= 256 && a.nu >= 8) return launch_tiles<T, NW, 2>(a, blocks, group, st);
-    return launch_tiles<T, NW, 1>(a, blocks, group, st);
+    auto blocks_of = [&](int NW) { return (long long)(a.H / a.dh) * ((all + NW - 1) / NW) * ((a.rows + 127) / 128); };
+    const long long narrow = blocks_of(2), wide = blocks_of(4);
+    if constexpr (sizeof(T) == 4) {
+        return launch_tiles<T, 4, 4, 1>(a, wide, group, st);
+    } else {
+        if (narrow <= 256 && a.nu >= 8) return launch_tiles<T, 4, 2, 2>(a, narrow, group, st);
+        if (wide >= (group == 32 ? 512 : 256) && 10 * wide <= 6 * narrow) return launch_tiles<T, 8, 4, 1>(a, wide, group, st);
+        return launch_tiles<T, 4, 2, 1>(a, narrow, group, st);
+    }
 }
 template <typename T, int NG, bool STEP> hipError_t launch_rows_of(RowsQ4Args a, int n_heads, int group, hipStream_t st)
 {
