@@ -94,7 +94,8 @@ __device__ __forceinline__ bool unit_of(const PrepArgs &a, long long *rt, int *k
     return *ku < a.per_row;
 }
 
-// A wave takes PER k units of 16 outputs: one, or the two that share a scale.  Memory-bound: 4.5 bytes a weight.
+// A wave takes PER k units of 16 outputs: one, or the two that share a scale.  Memory-bound, 4.53 bytes a weight: 30 us for 2 x 4096 x 4096
+// weights, 5.1 TB/s (vector issue 0.9 of the time, most of it the quotients, which are exact so that halves go to the even code).
 template <int PER> __global__ __launch_bounds__(256) void q4_quantize_kernel(const PrepArgs a)
 {
     long long rt;
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const PrepArgs a)
             if (k % a.group == 0) a.scales_out[(rt * ng + k / a.group) * 16 + n] = a.code_scales[(rt * 16 + n) * ng + k / a.group];
 }
 
-// Wx fp32, or rounded to bf16 for the matrix products of many rows
+// Wx fp32, or rounded to bf16 for the matrix products of many rows.  Memory-bound: 25 us for 2 x 4096 x 4096 weights to fp32, 6.0 TB/s.
 template <bool BF16> __global__ __launch_bounds__(256) void q4_dequantize_kernel(const PrepArgs a)
 {
     if (BF16 && blockIdx.x == 0 && threadIdx.x < 8) a.tickets[threadIdx.x] = 0;      // for the product that follows
@@ -242,6 +243,8 @@ template <> struct Eight<float> {
 // them and add up in LDS.  A row's inputs are read once for the NG CT tiles of weights and a weight once for the 16 MT rows.
 // Few rows are bound by the way to memory and back, so a wave asks for its units at once (its whole share of up to 4096 inputs for
 // one row), and for what it adds to the sums before the first of them comes.  G32: groups of 32 inputs, else of 64 and more.
+// One row, 3 x 4096 x 4096 weights (27 MB, not in a cache): 11 us, 2.4 TB/s; a step with 2 x 4096 x 4096 6.1, 2.9 TB/s;
+// launch, loads and sums of a small one 3.5 to 4.7 in a graph.
 template <typename T, int MT, int NG, int CT, bool STEP, bool G32>
 __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel(const RowsQ4Args a)
 {
@@ -470,9 +473,13 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
 }
 
 // ------------------------------------------------------------------ products of many rows
-// A workgroup: 128 rows x 64 NW channels of a gate, 2 x NW waves of 64 x 64 each that go through the inputs together, a unit at a time.  Rows come
-// into LDS once for all of them (fp32: as their three terms), two places in turn with one barrier a unit; weights go from
-// memory into the operand registers as above, the next unit's on their way meanwhile.
+// A workgroup: 128 rows x 64 NW channels of a head, waves of 16 MT rows x 64 channels that go through the inputs together, a unit at a time (KS = 2:
+// a unit each for two halves of the waves, whose sums are added in LDS).  Rows come into LDS once for all waves (fp32: as their three
+// terms), two places in turn with one barrier a unit; weights go from memory into the operand registers as above, the next unit's
+// on their way meanwhile.  Bound by instruction issue: for 64 x 64 x 64 a wave issues 40 matrix and 160 vector instructions, 64 of which
+// scale the sums of a group (MT = 8 halves those that unpack; groups of 128 are scaled by units too), and fp32 96 and 520.  0.80 PFLOP/s
+// with heads of 1024 inputs and 4096 rows, fp32 0.32; 0.55 at 1024 rows of 2816 x 4 x 704.  Without effect: loads two units ahead,
+// reads of LDS a step ahead, three waves a SIMD.
 template <typename T, int MT, int NW, int KS, bool G32>
 __global__ __launch_bounds__(64 * 8 / MT * NW * KS, 2) void q4_tiles_kernel(const RowsQ4Args a)
 {
