@@ -226,6 +226,34 @@ def test_step_is_captured(P):
         assert torch.equal(y, e_y) and torch.equal(h, e_h)
 
 
+@pytest.mark.parametrize("rows", [5, 200, 1700, -1])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_products_are_captured(P, rows, dtype):
+    """Replays on new inputs with eager calls between them and on another stream, for every way that the products take."""
+    G, heads, dh = (3, 1, 640) if rows > 0 else (8, 1, 2048)
+    rows = rows if rows > 0 else P.q4_exact_rows(dh, G, 1) + 5
+    Wq = P.quantize_projection(weights(G, heads, dh, seed=21).cuda(), n_heads=heads)
+    gen = torch.Generator(device="cuda").manual_seed(22)
+    x = torch.randn(1, rows, dh, generator=gen, device="cuda").to(dtype)
+    P.input_projection_q4(x, Wq)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        u = P.input_projection_q4(x, Wq)
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        x.copy_(torch.randn(1, rows, dh, generator=gen, device="cuda"))
+        graph.replay()
+        want = P.input_projection_q4(x, Wq)
+        assert torch.equal(u, want)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            other = P.input_projection_q4(x, Wq)
+        raw = P.input_projection_q4(x, Wq, stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(other, want) and torch.equal(raw, want)
+
+
 # ---------------------------------------------------------------- together
 def test_a_layer_from_training_to_serving(P):
     """A training step, the weights to 4 bits, a padded batch of prompts, then tokens: against the plain form of the 4-bit
