@@ -54,18 +54,25 @@ __device__ __forceinline__ bf8v operand(unsigned int w, unsigned int one)
     return __builtin_bit_cast(bf8v, r);
 }
 
-// the same less 24, exact too: for fp32, where the 24 and its product would cost the sums three bits
-__device__ __forceinline__ bf8v operand_signed(unsigned int w, unsigned int one)
+// q / 16 by table, exact: for fp32, where the 24 and its product would cost the sums three bits
+__device__ __forceinline__ bf8v operand_signed(unsigned int w)
 {
-    const u4v r = __builtin_bit_cast(u4v, operand(w, one));
-    u4v q;
+    const unsigned int even = w ^ 0x88888888u, odd = even >> 4;      // two's complement
+    u4v r;
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-        const unsigned int lo = __float_as_uint(__uint_as_float(r[p] << 16) - 24.0f);
-        const unsigned int hi = __float_as_uint(__uint_as_float(r[p] & 0xffff0000u) - 24.0f);
-        q[p] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);       // the upper halves of both
+        float lo, hi;
+        const unsigned int from = p & 1 ? odd : even;
+        if (p < 2) {
+            asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD src0_sel:BYTE_0" : "=v"(lo) : "v"(from));
+            asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD src0_sel:BYTE_2" : "=v"(hi) : "v"(from));
+        } else {
+            asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD src0_sel:BYTE_1" : "=v"(lo) : "v"(from));
+            asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD src0_sel:BYTE_3" : "=v"(hi) : "v"(from));
+        }
+        r[p] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);      // the upper halves of both
     }
-    return __builtin_bit_cast(bf8v, q);
+    return __builtin_bit_cast(bf8v, r);
 }
 
 struct PrepArgs {
@@ -225,17 +232,23 @@ template <> struct Eight<float> {
         c[0] = *reinterpret_cast<const u4v *>(p);
         c[1] = *reinterpret_cast<const u4v *>(p + 4);
     }
-    // x = t0 + t1 + t2: what a term leaves is exact in fp32, and eight bits of mantissa three times are all 24
+    // x = t0 + t1 + t2, cut off and not rounded: eight bits of mantissa three times are all 24, and what a term leaves is exact.  (An infinity
+    // leaves a NaN.)
     __device__ __forceinline__ void terms(bf8v (&t)[3]) const
     {
+        u4v r[3];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float x = __uint_as_float(c[e >> 2][e & 3]);
-            t[0][e] = (__bf16)x;
-            const float r = x - (float)t[0][e];
-            t[1][e] = (__bf16)r;
-            t[2][e] = (__bf16)(r - (float)t[1][e]);
+        for (int p = 0; p < 4; ++p) {
+            float x[2] = {__uint_as_float(c[p >> 1][2 * p & 3]), __uint_as_float(c[p >> 1][(2 * p & 3) + 1])};
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                r[k][p] = __builtin_amdgcn_perm(__float_as_uint(x[1]), __float_as_uint(x[0]), 0x07060302u);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) x[e] -= __uint_as_float(__float_as_uint(x[e]) & 0xffff0000u);
+            }
         }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) t[k] = __builtin_bit_cast(bf8v, r[k]);
     }
 };
 
@@ -316,8 +329,8 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
             for (int g = 0; g < NT; ++g) {
                 bf8v b[STEPS];
 #pragma unroll
-                for (int s = 0; s < STEPS; ++s) b[s] = TERMS == 1 ? operand(q[g][p * STEPS + s], one) : operand_signed(q[g][p * STEPS + s], one);
-                const float scale = __uint_as_float(sc[g][G32 ? p : 0] << 16);
+                for (int s = 0; s < STEPS; ++s) b[s] = TERMS == 1 ? operand(q[g][p * STEPS + s], one) : operand_signed(q[g][p * STEPS + s]);
+                const float scale = (TERMS == 1 ? 1.0f : 16.0f) * __uint_as_float(sc[g][G32 ? p : 0] << 16);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     f4v acc = start[m];
@@ -567,9 +580,9 @@ __global__ __launch_bounds__(64 * 8 / MT * NW * KS, 2) void q4_tiles_kernel(cons
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) b[c][s] = TERMS == 1 ? operand(q[c][s], one) : operand_signed(q[c][s], one);
-            scale[c][0] = __uint_as_float(sc[c][0] << 16);
-            if constexpr (G32) scale[c][1] = __uint_as_float(sc[c][1] << 16);
+            for (int s = 0; s < 2; ++s) b[c][s] = TERMS == 1 ? operand(q[c][s], one) : operand_signed(q[c][s]);
+            scale[c][0] = (TERMS == 1 ? 1.0f : 16.0f) * __uint_as_float(sc[c][0] << 16);
+            if constexpr (G32) scale[c][1] = (TERMS == 1 ? 1.0f : 16.0f) * __uint_as_float(sc[c][1] << 16);
         }
         load_weights(ku + KS);
         if (KS > 1 && ku >= a.nu) break;      // (the last round, and the barriers are behind)
