@@ -506,7 +506,7 @@ int pararnn_gated_backward(int dtype, const void *u, const float *checkpoints, c
  *   and is never written.  No workspace.
  * There are no gradients.  Device pointers; x 16-byte aligned (u too beyond pararnn_q4_exact_rows() rows of bf16), the others as
  * their elements.  A NaN or an infinity in x makes that row's outputs of that head NaN or infinite; so may finite inputs
- * beyond 1e36 in magnitude, whose products with the codes' operands overflow.
+ * or scales beyond 1e36 in magnitude, whose products overflow on the way.
  */
 size_t pararnn_q4_packed_bytes(int H, int G, int n_heads);
 size_t pararnn_q4_scale_bytes(int H, int G, int n_heads, int group);

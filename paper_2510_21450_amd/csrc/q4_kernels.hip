@@ -490,8 +490,8 @@ __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel
 // a unit each for two halves of the waves, whose sums are added in LDS).  Rows come into LDS once for all waves (fp32: as their three
 // terms), two places in turn with one barrier a unit; weights go from memory into the operand registers as above, the next unit's
 // on their way meanwhile.  Bound by instruction issue: for 64 x 64 x 64 a wave issues 40 matrix and 160 vector instructions, 64 of which
-// scale the sums of a group (MT = 8 halves those that unpack; groups of 128 are scaled by units too), and fp32 96 and 520.  0.80 PFLOP/s
-// with heads of 1024 inputs and 4096 rows, fp32 0.32; 0.55 at 1024 rows of 2816 x 4 x 704.  Without effect: loads two units ahead,
+// scale the sums of a group (MT = 8 halves those that unpack; groups of 128 are scaled by units too), and fp32 96 and 340.  0.80 PFLOP/s
+// with heads of 1024 inputs and 4096 rows, fp32 0.35; 0.57 at 1024 rows of 2816 x 4 x 704.  Without effect: loads two units ahead,
 // reads of LDS a step ahead, three waves a SIMD.
 template <typename T, int MT, int NW, int KS, bool G32>
 __global__ __launch_bounds__(64 * 8 / MT * NW * KS, 2) void q4_tiles_kernel(const RowsQ4Args a)
@@ -707,12 +707,12 @@ constexpr int kWorkgroups = 192;        // fewer leave too much of the device id
 // device.  bf16, 16 x 16 against 32 x 64 (a step: 32 x 16 of each gate): with 3 x 4096 x 4096 weights 11.1 us for one row and 16.1
 // for 16 against 11.8 and 12.0; a step with 2 x 8192 x 1024 5.7 and 6.9 against 5.6 and 5.7, with 2 x 4096 x 4096 7.3 and 9.3 against
 // 8.5 and 8.6; with too few workgroups, 3 x 2048 x 1024, 3.4 and 4.4 against 5.4 and 5.5.  fp32, whose terms cost more than the
-// weights: 21 and 27 against 24 and 24, 5.0 and 6.6 against 8.8 and 8.9.
+// weights: 4, 8 and 16 rows 17.3, 19.2 and 27.2 against 20.1, 19.4 and 19.4, a step with 2 x 4096 x 4096 10.5, 10.7 and 12.4 against 14.7.
 // Whether tiles of 128 rows beat the kernel of few rows.  They use a weight for twice the rows or more and need no sums of eight waves, but have
-// fewer workgroups, which take a unit in 0.7 us (fp32 3.1): it pays from a number of the latter's workgroups (64 rows x 64 channels,
+// fewer workgroups, which take a unit in 0.7 us (fp32 2.9): it pays from a number of the latter's workgroups (64 rows x 64 channels,
 // fp32 32 x 64) on.  Both level, bf16, units of a head: that number: 1: 90, 4: 340, 8: 300, 11: 340, 16: 390, 32: 580; 4096 rows: 9.9 to
-// 5.6 us, 32 to 18, 45 to 18, 245 to 97, 155 to 70, 146 to 88.  fp32: 6: 1000, 16: 1800 (512 rows 33 to 24, 94 to 54; 4096 rows 248 to 76, 730 to
-// 319), and not with too few of either (512 x 2 x 256: 2048 rows 12.2 to 16.9, 4096 22 to 18).
+// 5.6 us, 32 to 18, 45 to 18, 245 to 83, 155 to 64, 146 to 75.  fp32: 6: 1000, 16: 1800 (512 rows 29 to 21.5, 80 to 48; 4096 rows 215 to 72, 622 to
+// 298), and not with too few of either (512 x 2 x 256: 2048 rows 11.0 to 15, 4096 20.4 to 16.6).
 bool tiles_better(const RowsQ4Args &a, bool bf16)
 {
     if (a.rows <= 64) return false;
@@ -759,7 +759,7 @@ template <typename T, int NG, bool STEP> hipError_t launch_rows_of(RowsQ4Args a,
         if (tiles_better(a, bf16)) return launch_tiles<T>(a, group, st);
     if constexpr (bf16)
         if (a.rows > 32 && enough(4, C4)) return launch_rows<T, 4, NG, C4, STEP>(a, group, st);
-    if (a.rows > (bf16 ? 8 : 16) && enough(2, C4)) return launch_rows<T, 2, NG, C4, STEP>(a, group, st);
+    if (a.rows > (bf16 || !STEP ? 8 : 16) && enough(2, C4)) return launch_rows<T, 2, NG, C4, STEP>(a, group, st);
     if (a.rows > 16 && enough(2, 1)) return launch_rows<T, 2, NG, 1, STEP>(a, group, st);
     return launch_rows<T, 1, NG, 1, STEP>(a, group, st);
 }
