@@ -254,6 +254,16 @@ def test_products_are_captured(P, rows, dtype):
         assert torch.equal(other, want) and torch.equal(raw, want)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_offsets_beyond_32_bits(P, dtype):
+    """More than 2^31 outputs and 2^30 inputs: the last rows are what they are by themselves."""
+    Wq = P.quantize_projection(weights(2, 64, 64, seed=31).cuda(), n_heads=64)
+    x = torch.randn(1, 300000, 4096, device="cuda", generator=torch.Generator(device="cuda").manual_seed(32), dtype=dtype)
+    u = P.input_projection_q4(x, Wq)
+    assert u.numel() > 2 ** 31 and torch.equal(u[:, -5000:], P.input_projection_q4(x[:, -5000:], Wq))
+    assert torch.equal(u[:, :5000], P.input_projection_q4(x[:, :5000], Wq))
+
+
 # ---------------------------------------------------------------- together
 def test_a_layer_from_training_to_serving(P):
     """A training step, the weights to 4 bits, a padded batch of prompts, then tokens: against the plain form of the 4-bit
