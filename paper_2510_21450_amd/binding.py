@@ -26,7 +26,7 @@ try:
 except ImportError as e:
     raise ImportError(f"the native binding module beside {_LIB_PATH} is missing or unusable ({e}): build it with "
                       "`python -m paper_2510_21450_amd.build`") from e
-for _name in ("pararnn_input_projection", "pararnn_residual_norm", "pararnn_set_dense_jacobian", "pararnn_device_info", "pararnn_set_dense_products", "pararnn_solve_plan", "pararnn_affine_scan_workspace_bytes", "pararnn_gated_layer_step"):
+for _name in ("pararnn_input_projection", "pararnn_residual_norm", "pararnn_set_dense_jacobian", "pararnn_device_info", "pararnn_set_dense_products", "pararnn_solve_plan", "pararnn_affine_scan_workspace_bytes", "pararnn_gated_layer_step", "pararnn_set_q4_products"):
     if not hasattr(_lib, _name):
         raise ImportError(f"{_LIB_PATH} is older than this binding ({_name} is missing): rebuild it with "
                           "`python -m paper_2510_21450_amd.build`")
@@ -486,9 +486,15 @@ def input_projection_q4(x, Wq: ProjectionQ4, bias=None, workspace=None, stream=N
 
 
 def q4_exact_rows(H: int, G: int, n_heads: int = 1) -> int:
-    """pararnn_q4_exact_rows: rows B * L up to which `input_projection_q4` multiplies bf16 inputs with the 4-bit values themselves;
-    beyond, with the values rounded to bf16."""
+    """pararnn_q4_exact_rows: rows B * L up to which `input_projection_q4` multiplies bf16 inputs with the 4-bit values themselves
+    also under `set_q4_products(1)`."""
     return _lib.pararnn_q4_exact_rows(H, G, n_heads)
+
+
+def set_q4_products(mode: int = 0) -> None:
+    """pararnn_set_q4_products: 0 products with the 4-bit values whatever the number of rows (default), 1 with the values rounded to
+    bf16 for bf16 inputs of more than `q4_exact_rows` rows, which is faster."""
+    _raise(_lib.pararnn_set_q4_products(int(mode)), "pararnn_set_q4_products")
 
 
 def gated_layer_step(x, Wq: ProjectionQ4, h=None, bias=None, stream=None, out=None):

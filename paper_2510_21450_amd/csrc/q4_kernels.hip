@@ -10,6 +10,7 @@
 // Groups are scaled in fp32 as their sums are added up.  fp32 inputs are split into three bf16 terms (24 bits), and codes are
 // operands without the 24, whose sums would lose three of those bits.
 #include <algorithm>
+#include <atomic>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const PrepArgs a)
             if (k % a.group == 0) a.scales_out[(rt * ng + k / a.group) * 16 + n] = a.code_scales[(rt * 16 + n) * ng + k / a.group];
 }
 
-// Wx fp32, or rounded to bf16 for the matrix products of many rows.  Memory-bound: 25 us for 2 x 4096 x 4096 weights to fp32, 6.0 TB/s.
+// Wx fp32, or rounded to bf16 for the matrix products of many rows where the caller asks for those.  Memory-bound: 25 us for 2 x 4096 x 4096 weights to fp32, 6.0 TB/s.
 template <bool BF16> __global__ __launch_bounds__(256) void q4_dequantize_kernel(const PrepArgs a)
 {
     if (BF16 && blockIdx.x == 0 && threadIdx.x < 8) a.tickets[threadIdx.x] = 0;      // for the product that follows
@@ -650,8 +651,12 @@ __global__ __launch_bounds__(64 * 8 / MT * NW * KS, 2) void q4_tiles_kernel(cons
 }
 
 // ------------------------------------------------------------------ host
-// Rows up to which bf16 inputs are multiplied with the codes themselves; beyond, the weights are written out in bf16 for the tiles of the
-// projection, whose rate is higher but which start with that.  In units of what 256 of the projection's tiles (256 x 256) take: those
+// pararnn_set_q4_products: 0: products with the codes whatever the rows, 1: beyond exact_rows with the weights rounded to bf16
+std::atomic<int> g_products{0};
+
+// Rows from which the weights rounded to bf16 and written out for the tiles of the projection, whose rate is higher but which start with
+// that, are ahead of the codes themselves.  A weight has up to 11 significant bits and loses up to three of them, so a caller has to
+// ask for it: products of one layer would else see other weights in a long prompt than in the tokens after it.  In units of what 256 of the projection's tiles (256 x 256) take: those
 // take 8 us and, for every 256 tiles begun, 10 us and 1.4 for each 64 inputs of a head (2048 x 2 x 2048: 56 us for 65 rows, 61 for 2048,
 // 72 for 4096, 116 for 6000; 4096 x 3 x 1024: 41 to 45 up to 1024 rows, 73 for 2048, 106 for 4096); q4_tiles_kernel takes 2 us and 5 + 2.15 for
 // each 64 inputs, in proportion to the rows (46 us for 2048, 76 for 4096, 113 for 6000; 38, 64 and 120), with groups of 32 a fifth
@@ -817,6 +822,13 @@ int q4_dequantize(const void *packed, const void *scales, int H, int G, int n_he
     return hipGetLastError() == hipSuccess ? PARARNN_OK : PARARNN_HIP_ERROR;
 }
 
+int q4_set_products(int mode)
+{
+    if (mode < 0 || mode > 1) return PARARNN_INVALID_ARG;
+    g_products.store(mode, std::memory_order_relaxed);
+    return PARARNN_OK;
+}
+
 int q4_exact_rows(int H, int G, int n_heads)
 {
     return weights_ok(H, G, n_heads) && !unsupported(H, G, n_heads, 32) ? exact_rows(H, G, n_heads) : -1;
@@ -842,8 +854,9 @@ int q4_project(int dtype, const void *x, const void *packed, const void *scales,
     if (need == 0) return PARARNN_INVALID_ARG;
     if (workspace_bytes < need) return PARARNN_WORKSPACE_TOO_SMALL;
     const int rows = B * L;
-    if (dtype == PARARNN_BF16 && rows > exact_rows(H, G, n_heads)) {
-        if (misaligned(u, 16)) return PARARNN_UNSUPPORTED;
+    const bool many = dtype == PARARNN_BF16 && rows > exact_rows(H, G, n_heads);
+    if (many && misaligned(u, 16)) return PARARNN_UNSUPPORTED;      // (with either products, as the workspace: the choice may change between calls)
+    if (many && g_products.load(std::memory_order_relaxed) == 1) {
         int *tickets = nullptr;
         unsigned short *Wb = proj_weights_at(workspace, &tickets);
         PrepArgs p = prep_args(H, G, n_heads, group, 1);

@@ -121,6 +121,19 @@ def test_q4_refusals(lib):
     assert step(h=A + 2) == INVALID and step(nxt=A + 2) == INVALID and step(B=(1 << 20) + 1) == UNSUPPORTED
 
 
+def test_choice_of_products(lib):
+    """What a call asks of its workspace and of u is the same in either mode; other modes do not exist."""
+    few = lib.pararnn_q4_exact_rows(4096, 3, 1)
+    assert lib.pararnn_set_q4_products(-1) == INVALID and lib.pararnn_set_q4_products(2) == INVALID
+    asked = []
+    for mode in (0, 1, 0):
+        assert lib.pararnn_set_q4_products(mode) == 0
+        many = (BF16, A, A, A, A, 1, few + 1, 4096, 3, 1, 64)
+        asked.append((lib.pararnn_q4_exact_rows(4096, 3, 1), lib.pararnn_q4_workspace_bytes(BF16, 1, few + 1, 4096, 3, 1, 64),
+                      lib.pararnn_input_projection_q4(*many, A, A, 256, None), lib.pararnn_input_projection_q4(*many, A + 2, A, 1 << 30, None)))
+    assert asked[0] == asked[1] == asked[2] and asked[0][2:] == (TOO_SMALL, UNSUPPORTED)
+
+
 def test_python_refuses_what_is_not_on_the_gpu():
     torch = pytest.importorskip("torch")
     import paper_2510_21450_amd as P

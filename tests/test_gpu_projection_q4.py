@@ -139,6 +139,53 @@ def test_products_in_tiles(P, rows, G, heads, dh, group, dtype):
     assert torch.equal(u, again)
 
 
+def rounding_shows(G, dh, group, rows):
+    """codes, scales, x and bias whose products cancel: inputs 1 and -7 under codes 7 and 1 take each other out exactly, and 7 s of the scale
+    148 / 128 lies in the middle between two bf16 numbers: in bf16 each pair is off by 2^-5 of the inputs.  What is summed up are whole numbers
+    below 2^24 (times a power of two), so that fp32 sums in any order are exact and u is the bias, rounded."""
+    even = torch.arange(dh) % 2 == 0
+    codes = torch.where(even, 7, 1).to(torch.int8).expand(G, dh, dh).contiguous()
+    scales = torch.full((G, dh, dh // group), 148 / 128, dtype=torch.bfloat16)
+    x = torch.where(even, 1.0, -7.0) * 2.0 ** (torch.arange(rows) % 3).unsqueeze(1)
+    bias = torch.randn(G, dh, generator=torch.Generator().manual_seed(group))
+    return codes, scales, x.to(torch.bfloat16), bias
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("G,dh,beyond", [(3, 1024, -64), (3, 1024, 1), (3, 1024, 2500), (8, 2048, 5)])
+def test_any_number_of_rows_sees_the_weights(P, G, dh, beyond, group):
+    """A prompt of many rows is multiplied with the same weights as the tokens after it: none of them is rounded."""
+    rows = P.q4_exact_rows(dh, G, 1) + beyond
+    codes, scales, x, bias = rounding_shows(G, dh, group, rows)
+    Wq = P.pack_projection(codes.cuda(), scales.cuda())
+    u = P.input_projection_q4(x[None].cuda(), Wq, bias.cuda())
+    want = bias.to(torch.bfloat16).expand(1, rows, G, dh)
+    assert torch.equal(u.cpu(), want)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_rounded_weights_where_they_are_asked_for(P, group):
+    """set_q4_products(1): the weights rounded to bf16 from q4_exact_rows on, the codes up to there, and the codes again under 0."""
+    G, dh = 3, 1024
+    rows = P.q4_exact_rows(dh, G, 1)
+    codes, scales, x, bias = rounding_shows(G, dh, group, rows + 7)
+    Wq = P.pack_projection(codes.cuda(), scales.cuda())
+    call = lambda n: P.input_projection_q4(x[None, :n].contiguous().cuda(), Wq, bias.cuda())
+    exact = bias.to(torch.bfloat16)
+    # 512 pairs that are 2^-5 off each, times 1, 2 or 4: whole multiples of 2^-7 below 2^24 of them, exact sums as well
+    rounded = ref.project(x, ref.values(codes, scales).to(torch.bfloat16).double(), bias, 1)
+    try:
+        P.set_q4_products(1)
+        assert torch.equal(call(rows)[0].cpu(), exact.expand(rows, G, dh))
+        ref.check(call(rows + 7)[0], rounded, 4 * ref.EPS * rounded.abs(), "u")
+    finally:
+        P.set_q4_products(0)
+    assert torch.equal(call(rows + 7)[0].cpu(), exact.expand(rows + 7, G, dh))
+    for mode in (-1, 2):
+        with pytest.raises(RuntimeError):
+            P.set_q4_products(mode)
+
+
 def test_a_row_keeps_to_itself(P):
     """A NaN in one row, an infinity in another, both in one head: those rows of that head alone, in tiles as in single rows."""
     Wq = P.quantize_projection(weights(4, 3, 64, seed=9).cuda(), n_heads=3)
