@@ -104,8 +104,11 @@ void raise_if(int code, const std::string &what)
     if (code != 0)
         throw std::runtime_error(what + " failed: " + pararnn_status_string(code) + " (" + std::to_string(code) + ")");
 }
+// (a workspace of host memory or of another device would hand the kernels an address that is not theirs)
 Tensor workspace_of(size_t bytes, const Tensor &like, const OptTensor &given)
 {
+    if (has(given) && given->device() != like.device())
+        throw py::value_error("workspace must be on " + like.device().str() + ", got " + given->device().str());
     return has(given) ? *given : at::empty({(int64_t)(bytes > 256 ? bytes : 256)}, like.options().dtype(at::kByte));
 }
 
@@ -653,6 +656,7 @@ Tensor q4_project(const Tensor &x, const Q4 &q, const OptTensor &bias, const Opt
     if (has(bias)) check_on(*bias, "bias", at::kFloat, {q.G, q.H}, x);
     Tensor u = has(out) ? *out : at::empty({B, L, q.G, q.H}, x.options());
     check_on(u, "u", dt, {B, L, q.G, q.H}, x);
+    if (has(workspace)) check_on(*workspace, "workspace", at::kByte, {workspace->numel()}, x);
     const Tensor ws = workspace_of(pararnn_q4_workspace_bytes(code, B, L, q.H, q.G, q.heads, q.group), x, workspace);
     raise_if(pararnn_input_projection_q4(code, x.data_ptr(), q.packed.data_ptr(), q.scales.data_ptr(), static_cast<const float *>(ptr(bias)),
                                          B, L, q.H, q.G, q.heads, q.group, u.data_ptr(), ws.data_ptr(), (size_t)ws.numel(), on.stream()),

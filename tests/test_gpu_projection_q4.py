@@ -410,3 +410,23 @@ def test_refusals(P):
     flat = torch.zeros(2 * 256 + 1, device="cuda")
     with pytest.raises(RuntimeError):
         P.gated_layer_step(flat[1:].view(2, 256), Wq)
+
+
+def test_a_workspace_is_checked(P):
+    """Of host memory, or of another type: refused before anything is launched."""
+    Wq = P.quantize_projection(weights(2, 1, 128, seed=1).cuda())
+    W = weights(2, 1, 128, seed=1).cuda()
+    x = torch.zeros(1, 3, 128, device="cuda")
+    u = torch.zeros(1, 3, 2, 128, device="cuda")
+    host = torch.empty(1 << 20, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="workspace"):
+        P.input_projection_q4(x, Wq, workspace=host)
+    with pytest.raises(ValueError, match="workspace"):
+        P.input_projection_q4(x, Wq, workspace=torch.empty(1 << 20, device="cuda"))
+    with pytest.raises(ValueError, match="workspace"):
+        P.input_projection_q4(x, Wq, workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda")[::2])
+    with pytest.raises(ValueError, match="workspace"):
+        P.input_projection(x, W, workspace=host)
+    with pytest.raises(ValueError, match="workspace"):
+        P.input_projection_backward(x, W, u, workspace=host)
+    assert torch.equal(P.input_projection_q4(x, Wq, workspace=torch.empty(256, dtype=torch.uint8, device="cuda")), u)
