@@ -8,7 +8,7 @@
 #include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/custom_function.h>
-#include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/autograd/functions/accumulate_grad.h>
 #include <torch/csrc/utils/pybind.h>
 #include <torch/custom_class.h>
 
@@ -794,15 +794,15 @@ struct Layer : torch::autograd::Function<Layer> {
 // A backward pass that is captured into a graph while another graph, built on another stream, keeps the accumulators of the same
 // leaves alive: the engine would make that stream wait for the captured one, which draws it into the capture and ends the
 // process when the capture ends.  Refused before anything is launched; what this node returns is what it would wait for.
-void refuse_foreign_leaves(std::initializer_list<Tensor> inputs)
+// They are found by the node's own edges: its inputs need not be kept for it.
+void refuse_foreign_leaves()
 {
     const auto cur = c10::hip::getCurrentHIPStream();
     hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
     if (hipStreamIsCapturing(cur.stream(), &cap) != hipSuccess || cap == hipStreamCaptureStatusNone) return;
-    for (const Tensor &t : inputs) {
-        if (!t.defined() || !t.requires_grad() || !t.is_leaf()) continue;
-        const auto node = torch::autograd::impl::try_get_grad_accumulator(t);
-        const auto stream = node ? node->stream() : c10::nullopt;
+    for (const torch::autograd::Edge &e : torch::autograd::get_current_node()->next_edges()) {
+        if (!dynamic_cast<torch::autograd::AccumulateGrad *>(e.function.get())) continue;
+        const auto stream = e.function->stream();
         // (by number: the same stream is of another device type by name in either half of torch)
         if (stream && (stream->id() != cur.id() || stream->device_index() != cur.device_index()))
             throw std::runtime_error("a backward pass cannot be captured into a graph while an eager graph of the same leaves is alive: "
@@ -811,20 +811,21 @@ void refuse_foreign_leaves(std::initializer_list<Tensor> inputs)
 }
 
 // Gradients of a backward pass that itself is recorded (create_graph): the kernels' results have no history, so a node that says so
-// is put between them and what they depend on, and a derivative of them is an error in place of a missing term.
-void once(variable_list &out, const variable_list &inputs, const variable_list &grads)
+// is put between them and what they depend on, the inputs of the node they are of and its gradients, and a derivative of them is an
+// error in place of a missing term.
+struct NoSecond : torch::autograd::Node {
+    using Node::Node;
+    variable_list apply(variable_list &&) override { throw std::runtime_error("the gated recurrence has no second derivatives"); }
+};
+void once(variable_list &out, const variable_list &grads)
 {
     if (!at::GradMode::is_enabled()) return;
-    variable_list all(1);
-    for (const variable_list *from : {&inputs, &grads})
-        for (const Tensor &t : *from)
-            if (t.defined() && t.requires_grad()) all.push_back(t);
+    torch::autograd::edge_list on = torch::autograd::get_current_node()->next_edges();
+    for (const Tensor &t : grads)
+        if (t.defined() && t.requires_grad()) on.push_back(torch::autograd::impl::gradient_edge(t));
+    const auto node = std::make_shared<NoSecond>(std::move(on));
     for (Tensor &t : out)
-        if (t.defined()) {
-            all[0] = t;
-            auto refuse = std::make_shared<torch::autograd::DelayedError>("the gated recurrence has no second derivatives", (int64_t)all.size());
-            t = (*refuse)(variable_list(all))[0];
-        }
+        if (t.defined()) torch::autograd::create_gradient_edge(t, node);
 }
 
 // The gated linear recurrence: gated_forward with gated_backward as its gradient.
@@ -832,7 +833,8 @@ struct Gated : torch::autograd::Function<Gated> {
     static variable_list forward(AutogradContext *ctx, Tensor u, OptTensor h0, OptTensor lengths, bool train)
     {
         GatedOut r = gated_solve(u, h0, lengths, train, {}, {}, {}, {});
-        if (train) ctx->save_for_backward({u, r.ckpt, or_none(lengths), or_none(h0)});
+        if (train) ctx->save_for_backward({u, r.ckpt, or_none(lengths)});      // the states in front are in the checkpoints
+        ctx->saved_data["h0"] = has(h0);
         ctx->set_materialize_grads(false);
         return {r.h, r.last};
     }
@@ -841,13 +843,13 @@ struct Gated : torch::autograd::Function<Gated> {
         variable_list out(4);
         if (!grads[0].defined() && !grads[1].defined()) return out;
         const auto v = ctx->get_saved_variables();
-        refuse_foreign_leaves({v[0], v[3]});
+        refuse_foreign_leaves();
         Edges need{ctx};
         need(true);
-        const bool nh = need(v[3].defined());
+        const bool nh = need(ctx->saved_data["h0"].toBool());
         GatedGrads g = gated_adjoint(v[0], v[1], dense(grads[0]), dense(grads[1]), v[2], nh, {}, {}, {});
         out[0] = g.du; out[1] = g.dh0;
-        once(out, v, grads);
+        once(out, grads);
         return out;
     }
     static OptTensor dense(const Tensor &g) { return g.defined() ? OptTensor(g.contiguous()) : OptTensor(); }
@@ -863,8 +865,10 @@ struct GatedLayer : torch::autograd::Function<GatedLayer> {
             if (has(t) && t->device() != x.device()) throw py::value_error("x, Wx and bias must be on one device");
         Tensor u = project(x, Wx, bias, n_heads, {}, {}, {});
         GatedOut r = gated_solve(u, h0, lengths, train, {}, {}, {}, {});
-        if (train) ctx->save_for_backward({x, Wx, u, r.ckpt, or_none(lengths), or_none(bias), or_none(h0)});
+        if (train) ctx->save_for_backward({x, Wx, u, r.ckpt, or_none(lengths)});
         ctx->saved_data["n_heads"] = n_heads;
+        ctx->saved_data["bias"] = has(bias);
+        ctx->saved_data["h0"] = has(h0);
         ctx->set_materialize_grads(false);
         return {r.h, r.last};
     }
@@ -874,9 +878,9 @@ struct GatedLayer : torch::autograd::Function<GatedLayer> {
         if (!grads[0].defined() && !grads[1].defined()) return out;
         const auto v = ctx->get_saved_variables();
         const On on(v[0], "x", {});
-        refuse_foreign_leaves({v[0], v[1], v[5], v[6]});
+        refuse_foreign_leaves();
         Edges need{ctx};
-        const bool nx = need(true), nw = need(true), nb = need(v[5].defined()), nh = need(v[6].defined());
+        const bool nx = need(true), nw = need(true), nb = need(ctx->saved_data["bias"].toBool()), nh = need(ctx->saved_data["h0"].toBool());
         GatedGrads g = gated_adjoint(v[2], v[3], Gated::dense(grads[0]), Gated::dense(grads[1]), v[4], nh, {}, {}, {});
         out[3] = g.dh0;
         if (nx || nw || nb) {
@@ -885,7 +889,7 @@ struct GatedLayer : torch::autograd::Function<GatedLayer> {
             if (nw) out[1] = p.dW;
             out[2] = p.db;
         }
-        once(out, v, grads);
+        once(out, grads);
         return out;
     }
 };

@@ -477,6 +477,46 @@ def test_second_derivatives_are_refused(P, call):
             torch.autograd.grad(x.sum(), a, allow_unused=True)
 
 
+@pytest.mark.parametrize("call", ["layer", "apply"])
+@pytest.mark.parametrize("grad", [False, True])
+def test_what_the_backward_pass_does_not_read_may_be_overwritten(P, call, grad):
+    """A state buffer that takes the last state before the gradients are asked for, and a bias that an optimiser has stepped: the backward pass
+    works from the checkpoints, and its gradients are the same to the last bit."""
+    gen = torch.Generator().manual_seed(101)
+    x = torch.randn(2, 300, 64, generator=gen).to(torch.bfloat16).cuda().requires_grad_()
+    W = (torch.randn(2, 64, 64, generator=gen) / 8).cuda().requires_grad_()
+    u = torch.randn(2, 300, 2, 64, generator=gen).cuda().requires_grad_()
+    first, b = torch.randn(2, 64, generator=gen), torch.randn(2, 64, generator=gen)
+    g = torch.randn(2, 300, 64, generator=gen).to(torch.bfloat16 if call == "layer" else torch.float32).cuda()
+    got = []
+    for overwrite in (False, True):
+        state, bias = first.cuda().requires_grad_(grad), b.cuda().requires_grad_(grad)
+        h, last = P.gated_layer(x, W, bias, state) if call == "layer" else P.gated_apply(u, state)
+        if overwrite:
+            with torch.no_grad():
+                state.copy_(last)
+                bias.mul_(0.5)
+        leaves = ((x, W) if call == "layer" else (u,)) + ((state,) if grad else ()) + ((bias,) if grad and call == "layer" else ())
+        got.append(torch.autograd.grad(h, leaves, g))
+    assert all(torch.equal(p, q) for p, q in zip(*got))
+
+
+def test_second_derivatives_by_way_of_the_state(P):
+    """The gradients depend on the state in front and on the bias as well: a derivative of them with respect to those is an error too,
+    also where they are results of other operations."""
+    gen = torch.Generator().manual_seed(103)
+    x = torch.randn(2, 70, 64, generator=gen).cuda()
+    W = (torch.randn(2, 64, 64, generator=gen) / 8).cuda().requires_grad_()
+    g = torch.randn(2, 70, 64, generator=gen).cuda()
+    for leaf in (False, True):
+        s, b = torch.randn(2, 64, generator=gen).cuda().requires_grad_(), torch.randn(2, 64, generator=gen).cuda().requires_grad_()
+        h, _ = P.gated_layer(x, W, b if leaf else b * 2, s if leaf else s * 2)
+        dW, = torch.autograd.grad(h, W, g, create_graph=True)
+        for t in (s, b, W):
+            with pytest.raises(RuntimeError, match="second derivatives"):
+                torch.autograd.grad(dW.sum(), t, retain_graph=True)
+
+
 def test_threads(P):
     """Calls of two threads on one stream and on two, kept workspaces and all."""
     import threading
