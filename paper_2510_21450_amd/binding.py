@@ -269,8 +269,8 @@ def set_workspace_reuse(enable: bool = False) -> None:
 
 
 def release_workspaces() -> int:
-    """Give what `forward`, `backward` and the autograd functions keep of their workspaces between calls (at most 16 and a
-    thirty-second of the memory per device) back to torch's allocator; returns their bytes.  The allocator gets them back by
+    """Give what `forward`, `backward` and the autograd functions keep of their workspaces between calls (at most 16, 16 more of
+    the gated recurrence, and a thirty-second of the memory per device) back to torch's allocator; returns their bytes.  The allocator gets them back by
     itself before it takes more memory from the device."""
     return _host.release_workspaces()
 

@@ -41,6 +41,7 @@ struct Cell : torch::CustomClassHolder {
     std::string what;
     Ws ws_fn = nullptr, ws_fused_fn = nullptr;
     Parts parts_fn = nullptr;      // not in a library built before there was one
+    int (*tiles_fn)(int, int, int, int) = nullptr;      // tiles along L, where records depend on L by their number alone
     Fwd fwd_fn = nullptr;
     Bwd bwd_fn = nullptr;
 
@@ -121,14 +122,15 @@ struct Dims { int B, L, H; };
 // stream and problem, under the library's per-workspace promise; what nothing reads after the call (boundary rows, the fp32
 // iterate of bf16 storage, sums of parameter gradients: three quarters of a bf16 solve's workspace) is allocated for each
 // call as before.  A call takes a front out while it enqueues its work, and the next one that gets it is behind it in the
-// same stream; calls of several threads find different ones.  Bounds per device: kMost fronts and a thirty-second of its
+// same stream; calls of several threads find different ones.  Bounds per device: kMost fronts of the solvers, as many of the gated
+// recurrence (whose small ones would else push those out) and a thirty-second of its
 // memory, the least recently used go first, and all of them when torch's allocator would take more memory (GiveBack).  Under stream
 // capture, with a workspace or a stream of the caller's, for small problems (0.5 us of host time to look would show there; not
 // those of the gated recurrence, where clearing is a launch more) and for kernels without records nothing is kept.
 using WsKey = std::array<int64_t, 8>;
 constexpr size_t kMost = 16;
 constexpr double kSmall = 1 << 20;       // timestep-channels; below, most calls take kernels without records and 10-20 us
-struct KeptWs { WsKey key; Tensor ws; };
+struct KeptWs { WsKey key; Tensor ws; bool gated; };
 struct DevicePool {
     std::vector<KeptWs> free;          // least recently used first
     size_t bytes = 0, cap = 0;
@@ -200,12 +202,15 @@ public:
             std::lock_guard<std::mutex> lock(pool_mutex());
             DevicePool &p = pools()[device_];
             p.bytes += (size_t)ws_.numel();
-            p.free.push_back({key_, std::move(ws_)});
+            p.free.push_back({key_, std::move(ws_), gated_});
             kept_ = false;
-            while (p.free.size() > kMost || p.bytes > p.cap) {
-                p.bytes -= (size_t)p.free.front().ws.numel();
-                old.push_back(std::move(p.free.front()));
-                p.free.erase(p.free.begin());
+            const auto alike = [&](const KeptWs &k) { return k.gated == gated_; };
+            const auto too_many = [&] { return (size_t)std::count_if(p.free.begin(), p.free.end(), alike) > kMost; };
+            while (too_many() || p.bytes > p.cap) {
+                const auto k = too_many() ? std::find_if(p.free.begin(), p.free.end(), alike) : p.free.begin();
+                p.bytes -= (size_t)k->ws.numel();
+                old.push_back(std::move(*k));
+                p.free.erase(k);
             }
         }
         for (KeptWs &k : old) give_up(k.ws);
@@ -224,7 +229,8 @@ private:
         const size_t front = c.parts(code, d.B, d.L, d.H, back, (int)n_iters, rest);
         if (front == 0) return 0;
         key_ = {reinterpret_cast<int64_t>(cur.stream()), c.number >= 0 ? c.number : reinterpret_cast<int64_t>(c.fwd_fn),
-                back ? -1 : n_iters, code, d.B, d.L, d.H, (int64_t)front};
+                back ? -1 : n_iters, code, d.B, c.tiles_fn ? c.tiles_fn(code, d.B, d.L, d.H) : d.L, d.H, (int64_t)front};
+        gated_ = c.keeps_small;
         std::lock_guard<std::mutex> lock(pool_mutex());
         DevicePool &p = pools()[cur.device_index()];
         if (p.cap == 0) {
@@ -247,7 +253,7 @@ private:
     Tensor ws_, rest_;
     WsKey key_{};
     int device_ = -1;
-    bool kept_ = false;
+    bool kept_ = false, gated_ = false;
 };
 
 // Gives up what is kept on the current device; returns its bytes.
@@ -490,6 +496,9 @@ const Cell &gated_cell()
         r->parts_fn = [](int dtype, int B, int L, int H, int, int, size_t *rest) {
             *rest = 0;
             return pararnn_gated_workspace_bytes(dtype, B, L, H, 2);
+        };
+        r->tiles_fn = [](int dtype, int B, int L, int H) {   // a checkpoint for each, B x H fp32 numbers
+            return (int)(pararnn_gated_checkpoint_bytes(dtype, B, L, H, 2) / 4 / B / H);
         };
         return r;
     }();

@@ -1,4 +1,5 @@
 """The gated linear recurrence (forward, adjoint, autograd) on the GPU against plain 64-bit forms on the CPU."""
+import ctypes
 import gc
 
 import pytest
@@ -294,6 +295,48 @@ def test_captured(P):
         e_du, e_dh0 = P.gated_backward(u, e_ckpt, g, d, lengths=n)
         for a, b in ((h, e_h), (last, e_last), (du, e_du), (dh0, e_dh0)):
             assert torch.equal(a, b)
+
+
+def kept(P):
+    """Addresses of the workspaces whose records the library knows."""
+    known = ctypes.CDLL(P.lib_path()).pararnn_workspace_known
+    torch.cuda.synchronize()
+    return {b["address"] for s in torch.cuda.memory_snapshot() for b in s["blocks"]
+            if b["state"] == "active_allocated" and known(ctypes.c_void_p(b["address"]))}
+
+
+def test_gated_calls_have_places_of_their_own(P):
+    """More lengths than there are places do not push out what the solvers keep."""
+    P.release_workspaces()
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda")
+    # (weights of which the solve is finite: equal bits say something)
+    params = (torch.rand(2, 3, 260, generator=gen, device="cuda") * 2 - 1) * 0.9
+    u, h0, g = rand(2, 2100, 3, 260), 0.1 * rand(2, 1, 260), rand(2, 2100, 1, 260)
+
+    def solve():
+        h = P.forward("gru_diag", params, u, h0, tol=1e-5, max_iter=16)[0]
+        return (h, *P.backward("gru_diag", params, u, h0, h, g))
+    want = solve()
+    theirs = kept(P)
+    assert theirs
+    for tiles in range(2, 24):
+        P.gated_forward(rand(2, tiles * 128, 2, 64))
+    assert theirs <= kept(P) and 0 < len(kept(P) - theirs) <= 16
+    assert all(torch.equal(a, b) for a, b in zip(want, solve()))
+    P.release_workspaces()
+
+
+def test_lengths_of_as_many_tiles_share_a_workspace(P):
+    """Records depend on the tiles, not on the length: prompts that differ by a few steps use what the last one left."""
+    P.release_workspaces()
+    problems = [[cuda(t) for t in problem(2, L, 72, 2, torch.float32, seed=L)] for L in (1530, 1531, 1409, 1536)]
+    want = [both(P, *c, workspace=torch.empty(P.gated_workspace_bytes(torch.float32, 2, c[0].shape[1], 72, 2), dtype=torch.uint8, device="cuda"))
+            for c in problems]
+    for k in (0, 1, 2, 3, 0):
+        assert all(torch.equal(a, b) for a, b in zip(want[k], both(P, *problems[k]))), k
+        assert len(kept(P)) == 1
+    assert P.release_workspaces() == P.gated_workspace_bytes(torch.float32, 2, 1530, 72, 2)
 
 
 # ---------------------------------------------------------------- autograd
