@@ -465,7 +465,8 @@ int pararnn_input_projection_backward(int dtype, const void *x, const float *Wx,
  * Gradients, with lam_l the gradient of h_l: lam_l = g_l + f_{l+1} lam_{l+1} (+ dL_dlast behind the
  * last step), dv = lam i, du_i = lam v i (1 - i), du_f = lam h_{l-1} f (1 - f), for G = 2
  * du_f = lam (h_{l-1} - v) f (1 - f), dL_dh0 = f_1 lam_1.
- * Arithmetic in fp32; h and dL_du are rounded once.  Results are bit-reproducible.  Tensors need
+ * Arithmetic in fp32; h and dL_du are rounded once.  Results are bit-reproducible.  An infinite v, g or state is
+ * infinite from there on, and a NaN a NaN, in its channel alone.  (u_f = -inf leaves f at 2^-126.)  Tensors need
  * the alignment of their elements; an even H and the alignment of two are faster.  H <= 1 048 576,
  * B * H < 2^32 and less than 2^23 tiles, of 64 channels x 128 timesteps or 16 x 512 (H <= 32, some of few tiles; else UNSUPPORTED).  A wait that
  * runs out (see pararnn_set_spin_limit; it takes a broken promise for the workspace) gives NaN from there on.  Any number

@@ -118,6 +118,15 @@ __device__ __forceinline__ void sigmoid2(float x, float *f, float *one_minus)
     *one_minus = e * *f;
 }
 
+// The factor of a stretch's map.  Every gate is above 0, so a product of them that underflows is held at the least fp32 number in place of 0:
+// an infinite state or gradient stays one behind the stretch, as it does step by step, where 0 times it would be NaN.  What that adds is below
+// 2^-149 of the state.  (As whole numbers, where a NaN is larger than all that is compared here; one instruction.)
+__device__ __forceinline__ float factor(float a)
+{
+    const unsigned int w = __float_as_uint(a);
+    return __uint_as_float(w > 1u ? w : 1u);
+}
+
 // ------------------------------------------------------------------ carry records
 // Three 64-bit words {value, tag} for a tile and channel: A and S of the tile's map, and the state behind it.  A word is written
 // and read whole and validates itself (tag = number of the call and state), so no fence is needed.
@@ -330,6 +339,8 @@ __global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a
             S[k] = fmaf(f[j][k], S[k], b[j][k]);
         }
     }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) A[k] = factor(A[k]);
     // maps of the wave's segments up to and including this one, then without it
 #pragma unroll
     for (int d = LPR; d < 64; d *= 2)
@@ -337,7 +348,7 @@ __global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a
         for (int k = 0; k < VEC; ++k) {
             const float a1 = __shfl_up(A[k], d, 64), s1 = __shfl_up(S[k], d, 64);
             S[k] = fmaf(A[k], lane >= d ? s1 : 0.0f, S[k]);
-            A[k] *= lane >= d ? a1 : 1.0f;
+            A[k] = factor(A[k] * (lane >= d ? a1 : 1.0f));
         }
     if (sg == SEG - 1)
 #pragma unroll
@@ -362,12 +373,18 @@ __global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a
     for (int q = 0; q < w; ++q)
 #pragma unroll
         for (int k = 0; k < VEC; ++k) { ps[k] = fmaf(s_a[q][c0 + k], ps[k], s_s[q][c0 + k]); pa[k] *= s_a[q][c0 + k]; }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {                          // of all steps of the tile in front of this thread's
+        S[k] = fmaf(A[k], ps[k], S[k]);
+        A[k] = factor(A[k] * pa[k]);
+    }
     const bool more = LOOK && p.lt + 1 < a.n_lt;
     word_t *rec = a.rec + ((size_t)p.chain * a.n_lt + p.lt) * (3 * CW);
     float ta = 1.0f, ts = 0.0f;
     if (w == 0 && lane < CW) {
 #pragma unroll
         for (int q = 0; q < W; ++q) { ts = fmaf(s_a[q][lane], ts, s_s[q][lane]); ta *= s_a[q][lane]; }
+        ta = factor(ta);
         if (more && act && p.lt > 0) { put(rec + lane, ta, a.tag + 1); put(rec + CW + lane, ts, a.tag + 1); }
     }
     int found = -1, parity = 0;
@@ -389,7 +406,7 @@ __global__ __launch_bounds__(64 * W) void gated_forward_kernel(const GatedArgs a
     }
     entering(c0, x);
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) x[k] = fmaf(A[k], fmaf(pa[k], x[k], ps[k]), S[k]);
+    for (int k = 0; k < VEC; ++k) x[k] = fmaf(A[k], x[k], S[k]);
 
     const unsigned int at_out = unknown(at_h);
     const buf_rsrc rh = rsrc_of(static_cast<T *>(a.h) + row * H + first, extent(p.rows_all, H * es, first * es));
@@ -484,7 +501,7 @@ __global__ __launch_bounds__(64 * W, 4) void gated_backward_kernel(const GatedAr
             }
         }
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) RA[k] = A[k];
+    for (int k = 0; k < VEC; ++k) RA[k] = A[k] = factor(A[k]);
     // along time for the states, against it for the adjoint
 #pragma unroll
     for (int d = LPR; d < 64; d *= 2)
@@ -493,9 +510,9 @@ __global__ __launch_bounds__(64 * W, 4) void gated_backward_kernel(const GatedAr
             const float a1 = __shfl_up(A[k], d, 64), s1 = __shfl_up(S[k], d, 64);
             const float a2 = __shfl_down(RA[k], d, 64), m2 = __shfl_down(M[k], d, 64);
             S[k] = fmaf(A[k], lane >= d ? s1 : 0.0f, S[k]);
-            A[k] *= lane >= d ? a1 : 1.0f;
+            A[k] = factor(A[k] * (lane >= d ? a1 : 1.0f));
             M[k] = fmaf(RA[k], lane + d < 64 ? m2 : 0.0f, M[k]);
-            RA[k] *= lane + d < 64 ? a2 : 1.0f;
+            RA[k] = factor(RA[k] * (lane + d < 64 ? a2 : 1.0f));
         }
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
@@ -524,6 +541,7 @@ __global__ __launch_bounds__(64 * W, 4) void gated_backward_kernel(const GatedAr
     if (w == 0 && lane < CW) {
 #pragma unroll
         for (int q = W - 1; q >= 0; --q) { tm = fmaf(s_a[q][lane], tm, s_m[q][lane]); ta *= s_a[q][lane]; }
+        ta = factor(ta);
         if (more && act && p.lt + 1 < a.n_lt) { put(rec + lane, ta, a.tag + 1); put(rec + CW + lane, tm, a.tag + 1); }
     }
     // the state in front of each of this thread's steps
@@ -547,6 +565,8 @@ __global__ __launch_bounds__(64 * W, 4) void gated_backward_kernel(const GatedAr
     for (int q = W - 1; q > w; --q)
 #pragma unroll
         for (int k = 0; k < VEC; ++k) { pm[k] = fmaf(s_a[q][c0 + k], pm[k], s_m[q][c0 + k]); pa[k] *= s_a[q][c0 + k]; }
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) pa[k] = factor(pa[k]);
     int found = -1, parity = 0;
     if constexpr (LOOK)
         if (p.lt + 1 < a.n_lt) found = look_back(s_seen, rec, 1, p.lt, a.n_lt, act, a.tag, a.spin_limit, &parity);

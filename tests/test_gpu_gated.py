@@ -140,6 +140,37 @@ def test_nan_stays_where_it_belongs(P):
     assert torch.equal(torch.isnan(du).cpu(), want) and torch.isnan(dh0).cpu().nonzero().tolist() == [[1, 5]]
 
 
+def check_infinite(got, want, err, name):
+    """Infinities where the 64-bit form has them, with its signs, and its values elsewhere."""
+    got, far = got.double().cpu(), want.isinf()
+    assert not want.isnan().any() and torch.equal(got[far], want[far]), f"{name}: infinities"
+    half = ref.HALF_STEP[torch.bfloat16] if name.endswith("bf16") else ref.HALF_STEP[torch.float32]
+    assert ((got - want).abs() <= err * (1 + half) + half * want.abs() + 1e-37)[~far].all(), name
+
+
+@pytest.mark.parametrize("G", [2, 3])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,L,H", [(2, 5, 24), (2, 30, 24), (2, 128, 24), (2, 300, 33), (1, 700, 24), (1, 2100, 16), (1, 1700, 40)])
+def test_infinities_stay(P, B, L, H, dtype, G):
+    """An infinite v, g or h0 is infinite from there on, as step by step: memories here fall below the least fp32 number within tens of steps,
+    and a stretch's map must not turn an infinity into a NaN for it.  Other channels keep their values."""
+    u, h0, g, d = problem(B, L, H, G, dtype, seed=L + H)
+    u[:, :, 0] -= 4.5
+    for k, x in enumerate((float("inf"), float("-inf"))):
+        u[0, L // 3, -1, k] = x
+        g[0, L // 2, 2 + k] = x
+        h0[0, 4 + k] = x
+        d[0, 6 + k] = x
+    h, last, ckpt = P.gated_forward(u.cuda(), h0.cuda(), checkpoints=True)
+    du, dh0 = P.gated_backward(u.cuda(), ckpt, g.cuda(), d.cuda())
+    w, b = ref.forward(u, h0), ref.backward(u, h0, g, d)
+    low = " bf16" if dtype == torch.bfloat16 else ""
+    check_infinite(h, w[0], w[2], "h" + low)
+    check_infinite(last, w[1], w[3], "h_last")
+    check_infinite(du, b[0], b[2], "dL_du" + low)
+    check_infinite(dh0, b[1], b[3], "dL_dh0")
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_sequences_continue(P, dtype):
     """A sequence in pieces, the state updated in place, and token by token at its end: the states of the whole."""
