@@ -186,6 +186,52 @@ def test_rounded_weights_where_they_are_asked_for(P, group):
             P.set_q4_products(mode)
 
 
+def low_bits(rows, G, heads, dh, group, seed):
+    """fp32 inputs whose products cancel down to the last of their three bf16 terms.  Neighbours under the same code are a and -b with a, b of
+    65792 + {0, 1}: the terms 65536, 256 and 0 or 1, the first two the same in both.  Sums of code times x are whole numbers below
+    8 x 65793 x 16 < 2^24 for the 16 pairs of any 32 inputs, and those of all pairs below 8 dh / 2 < 2^24 once the pairs are whole, so fp32 sums
+    in any order are exact; scales are powers of two.  Without the third terms u would be 0."""
+    gen = torch.Generator().manual_seed(seed)
+    H = heads * dh
+    x = (65792.0 + torch.randint(0, 2, (rows, H), generator=gen)) * torch.tensor([1.0, -1.0]).repeat(H // 2)
+    codes = torch.randint(-8, 8, (G, H, dh // 2), generator=gen, dtype=torch.int8).repeat_interleave(2, -1)
+    scales = (2.0 ** torch.randint(-3, 3, (G, H, 1), generator=gen)).expand(G, H, dh // group).to(torch.bfloat16).contiguous()
+    return x, codes, scales
+
+
+def two_terms(x):
+    upper = lambda t: (t.view(torch.int32) & -65536).view(torch.float32)
+    return upper(x) + upper(x - upper(x))
+
+
+@pytest.mark.parametrize("rows,G,heads,dh,group", [(1, 2, 1, 64, 32), (3, 3, 2, 128, 128), (16, 1, 1, 640, 64), (16, 3, 1, 4096, 64), (20, 2, 1, 192, 32),
+                                                   (64, 4, 3, 192, 64), (2100, 4, 3, 64, 64), (900, 3, 5, 192, 32), (1153, 8, 1, 512, 128)])
+def test_every_bit_of_fp32_inputs_counts(P, rows, G, heads, dh, group):
+    x, codes, scales = low_bits(rows, G, heads, dh, group, seed=rows + dh)
+    V = ref.values(codes, scales)
+    want = ref.project(x, V, None, heads)
+    assert (ref.project(two_terms(x), V, None, heads) == 0).all() and (want != 0).double().mean() > 0.8
+    u = P.input_projection_q4(x[None].cuda(), P.pack_projection(codes.cuda(), scales.cuda(), n_heads=heads))
+    assert torch.equal(u.view(rows, G, -1).double().cpu(), want)
+
+
+@pytest.mark.parametrize("B,G,heads,dh,group", [(1, 2, 1, 256, 32), (5, 3, 2, 128, 128), (20, 2, 1, 640, 64), (64, 3, 1, 512, 64)])
+def test_every_bit_of_fp32_inputs_counts_in_a_step(P, B, G, heads, dh, group):
+    """v alone has codes that are not zero: f and i are sig(bias) and h' = f h + i v, to the gates' and three more roundings."""
+    x, codes, scales = low_bits(B, G, heads, dh, group, seed=B + dh)
+    codes[:-1] = 0
+    H = heads * dh
+    bias = torch.randn(G, H, generator=torch.Generator().manual_seed(B)).clamp(-ref.XMAX, ref.XMAX)
+    bias[-1] = 0
+    h = torch.randn(B, H, generator=torch.Generator().manual_seed(dh))
+    f, i, v = ref.gates(ref.project(x, ref.values(codes, scales), bias, heads))
+    mag = f * h.double().abs() + i * v.abs()
+    y, nxt = P.gated_layer_step(x.cuda(), P.pack_projection(codes.cuda(), scales.cuda(), n_heads=heads), h.cuda(), bias.cuda())
+    assert (v != 0).double().mean() > 0.8
+    ref.check(nxt, f * h.double() + i * v, (ref.GATE + 3) * ref.EPS * mag, "h_next")
+    assert torch.equal(y, nxt)
+
+
 def test_a_row_keeps_to_itself(P):
     """A NaN in one row, an infinity in another, both in one head: those rows of that head alone, in tiles as in single rows."""
     Wq = P.quantize_projection(weights(4, 3, 64, seed=9).cuda(), n_heads=3)
