@@ -171,6 +171,14 @@ def test_infinities_stay(P, B, L, H, dtype, G):
     check_infinite(dh0, b[1], b[3], "dL_dh0")
 
 
+@pytest.mark.parametrize("G", [2, 3])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,L,H", [(1, 1500, 64), (2, 1300, 130), (1, 4500, 66), (1, 17500, 16), (1, 17000, 31)])
+def test_looks_far_back(P, B, L, H, dtype, G):
+    """Looks of 32 tiles by one and by two channels a thread, one and more trips of them, and of narrow tiles."""
+    run_and_check(P, *problem(B, L, H, G, dtype, seed=B + L + H))
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_sequences_continue(P, dtype):
     """A sequence in pieces, the state updated in place, and token by token at its end: the states of the whole."""
@@ -241,6 +249,30 @@ def test_a_wait_that_runs_out(P):
     assert ok.all()
     again = both(P, *c)
     assert all(torch.equal(a, b) for a, b in zip(want, again))
+
+
+def test_what_a_wait_that_runs_out_leaves(P):
+    """Every output of both directions is right or NaN, and some of each is NaN: 235 tiles that are on the device together and wait for one
+    another look once."""
+    u, h0, g, d = [cuda(t) for t in problem(1, 30000, 64, 2, torch.float32, seed=19)]
+    h, last, ckpt = P.gated_forward(u, h0, checkpoints=True)
+    want = P.gated_backward(u, ckpt, g, d)
+    try:
+        P.set_spin_limit(1)
+        got = P.gated_forward(u, h0, checkpoints=True)
+        back = P.gated_backward(u, ckpt, g, d)               # its waits alone: from right checkpoints
+        from_bad = P.gated_backward(u, got[2], g, d)
+        torch.cuda.synchronize()
+    finally:
+        P.set_spin_limit(0)
+    pairs = list(zip(got, (h, last, ckpt))) + list(zip(back, want)) + list(zip(from_bad, want))
+    for k, (a, b) in enumerate(pairs):
+        assert ((a == b) | a.isnan()).all(), k
+    assert got[0].isnan().any() and got[2].isnan().any() and back[0].isnan().any() and from_bad[0].isnan().any()
+    # gradients of tiles whose checkpoint was not there need the state: not right by chance
+    lost = got[2][0].isnan()
+    assert from_bad[0][0, :, 0][lost[torch.arange(30000, device="cuda") // 128]].isnan().all()
+    assert all(torch.equal(a, b) for a, b in zip(P.gated_backward(u, ckpt, g, d), want))
 
 
 def scan_of_channels(u, h0):
