@@ -498,11 +498,12 @@ int pararnn_gated_backward(int dtype, const void *u, const float *checkpoints, c
  * pararnn_q4_dequantize: Wx fp32 [G][H][dh], code * scale (exact in fp32).
  * pararnn_input_projection_q4: u = B x + bias (bias fp32 [G][H] or NULL) for any number of rows.
  *   Products with the codes are exact, sums in fp32; fp32 storage: x in full (three bf16 terms).  workspace:
- *   pararnn_q4_workspace_bytes() bytes (0 on invalid arguments), 256-byte aligned.
+ *   pararnn_q4_workspace_bytes() bytes (0 on invalid arguments), 256-byte aligned, or NULL where no weights are rounded:
+ *   nothing else uses it.
  * pararnn_set_q4_products (host, process-wide; default 0): 0 as above; 1 allows bf16 storage of more than
  *   pararnn_q4_exact_rows() rows B * L to take weights rounded to bf16 (as pararnn_input_projection rounds its own), written
- *   into the workspace, and its matrix products, which are faster there.  What the call asks of its workspace and of u's alignment
- *   is the same in either mode.  INVALID_ARG for any other mode.
+ *   into the workspace, and its matrix products, which are faster there.  What the call asks of a workspace and of u's alignment
+ *   is the same in either mode.  INVALID_ARG for any other mode.  pararnn_q4_products: the present one.
  * pararnn_gated_layer_step: one token of a gated layer in one launch: the projection followed by one step
  *   of the gated linear recurrence, h' = f h + i v with G = 2 or 3 as there.  x, y [B][H] in the storage
  *   type, h, h_next fp32 [B][H] (may be the same memory; h NULL = zeros), y = h' rounded.  u stays in fp32
@@ -520,6 +521,7 @@ int pararnn_q4_pack(const signed char *codes, const void *code_scales, int H, in
 int pararnn_q4_dequantize(const void *packed, const void *scales, int H, int G, int n_heads, int group, float *Wx,
                           void *hip_stream);
 int pararnn_set_q4_products(int mode);
+int pararnn_q4_products(void);
 int pararnn_q4_exact_rows(int H, int G, int n_heads);
 size_t pararnn_q4_workspace_bytes(int dtype, int B, int L, int H, int G, int n_heads, int group);
 int pararnn_input_projection_q4(int dtype, const void *x, const void *packed, const void *scales, const float *bias,

@@ -666,9 +666,13 @@ Tensor q4_project(const Tensor &x, const Q4 &q, const OptTensor &bias, const Opt
     Tensor u = has(out) ? *out : at::empty({B, L, q.G, q.H}, x.options());
     check_on(u, "u", dt, {B, L, q.G, q.H}, x);
     if (has(workspace)) check_on(*workspace, "workspace", at::kByte, {workspace->numel()}, x);
-    const Tensor ws = workspace_of(pararnn_q4_workspace_bytes(code, B, L, q.H, q.G, q.heads, q.group), x, workspace);
+    // (two bytes a weight, which only rounded weights use)
+    Tensor ws = has(workspace) ? *workspace : Tensor();
+    if (!ws.defined() && pararnn_q4_products() == 1)
+        ws = workspace_of(pararnn_q4_workspace_bytes(code, B, L, q.H, q.G, q.heads, q.group), x, {});
     raise_if(pararnn_input_projection_q4(code, x.data_ptr(), q.packed.data_ptr(), q.scales.data_ptr(), static_cast<const float *>(ptr(bias)),
-                                         B, L, q.H, q.G, q.heads, q.group, u.data_ptr(), ws.data_ptr(), (size_t)ws.numel(), on.stream()),
+                                         B, L, q.H, q.G, q.heads, q.group, u.data_ptr(), ws.defined() ? ws.data_ptr() : nullptr,
+                                         ws.defined() ? (size_t)ws.numel() : 0, on.stream()),
              "pararnn_input_projection_q4");
     return u;
 }

@@ -641,6 +641,8 @@ int pararnn_q4_dequantize(const void *packed, const void *scales, int H, int G, 
 
 int pararnn_set_q4_products(int mode) { return q4_set_products(mode); }
 
+int pararnn_q4_products(void) { return q4_products(); }
+
 int pararnn_q4_exact_rows(int H, int G, int n_heads) { return q4_exact_rows(H, G, n_heads); }
 
 size_t pararnn_q4_workspace_bytes(int dtype, int B, int L, int H, int G, int n_heads, int group)

@@ -12,6 +12,7 @@ int q4_pack(const signed char *codes, const void *code_scales, int H, int G, int
             hipStream_t st);
 int q4_dequantize(const void *packed, const void *scales, int H, int G, int n_heads, int group, float *Wx, hipStream_t st);
 int q4_set_products(int mode);
+int q4_products();
 int q4_exact_rows(int H, int G, int n_heads);
 size_t q4_workspace_bytes(int dtype, int B, int L, int H, int G, int n_heads, int group);
 int q4_project(int dtype, const void *x, const void *packed, const void *scales, const float *bias, int B, int L, int H, int G,

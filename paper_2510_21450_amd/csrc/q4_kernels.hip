@@ -829,6 +829,8 @@ int q4_set_products(int mode)
     return PARARNN_OK;
 }
 
+int q4_products() { return g_products.load(std::memory_order_relaxed); }
+
 int q4_exact_rows(int H, int G, int n_heads)
 {
     return weights_ok(H, G, n_heads) && !unsupported(H, G, n_heads, 32) ? exact_rows(H, G, n_heads) : -1;
@@ -846,17 +848,18 @@ int q4_project(int dtype, const void *x, const void *packed, const void *scales,
 {
     const size_t es = dtype == PARARNN_BF16 ? 2 : 4;
     if ((dtype != PARARNN_F32 && dtype != PARARNN_BF16) || B < 1 || L < 1 || !weights_ok(H, G, n_heads) || !group_ok(group) || !x ||
-        !packed || !scales || !u || !workspace || misaligned(x, 16) || misaligned(packed, 16) || misaligned(scales, 2) ||
+        !packed || !scales || !u || misaligned(x, 16) || misaligned(packed, 16) || misaligned(scales, 2) ||
         misaligned(bias, 4) || misaligned(u, es) || misaligned(workspace, 256))
         return PARARNN_INVALID_ARG;
     if (unsupported(H, G, n_heads, group)) return PARARNN_UNSUPPORTED;
     const size_t need = q4_workspace_bytes(dtype, B, L, H, G, n_heads, group);
     if (need == 0) return PARARNN_INVALID_ARG;
-    if (workspace_bytes < need) return PARARNN_WORKSPACE_TOO_SMALL;
     const int rows = B * L;
-    const bool many = dtype == PARARNN_BF16 && rows > exact_rows(H, G, n_heads);
+    const bool many = dtype == PARARNN_BF16 && rows > exact_rows(H, G, n_heads), rounded = many && q4_products() == 1;
+    if (rounded && !workspace) return PARARNN_INVALID_ARG;
+    if (workspace && workspace_bytes < need) return PARARNN_WORKSPACE_TOO_SMALL;
     if (many && misaligned(u, 16)) return PARARNN_UNSUPPORTED;      // (with either products, as the workspace: the choice may change between calls)
-    if (many && g_products.load(std::memory_order_relaxed) == 1) {
+    if (rounded) {
         int *tickets = nullptr;
         unsigned short *Wb = proj_weights_at(workspace, &tickets);
         PrepArgs p = prep_args(H, G, n_heads, group, 1);

@@ -132,6 +132,11 @@ def test_choice_of_products(lib):
         asked.append((lib.pararnn_q4_exact_rows(4096, 3, 1), lib.pararnn_q4_workspace_bytes(BF16, 1, few + 1, 4096, 3, 1, 64),
                       lib.pararnn_input_projection_q4(*many, A, A, 256, None), lib.pararnn_input_projection_q4(*many, A + 2, A, 1 << 30, None)))
     assert asked[0] == asked[1] == asked[2] and asked[0][2:] == (TOO_SMALL, UNSUPPORTED)
+    try:
+        assert lib.pararnn_set_q4_products(1) == 0 and lib.pararnn_q4_products() == 1
+        assert lib.pararnn_input_projection_q4(BF16, A, A, A, A, 1, few + 1, 4096, 3, 1, 64, A, None, 0, None) == INVALID
+    finally:
+        assert lib.pararnn_set_q4_products(0) == 0 and lib.pararnn_q4_products() == 0
 
 
 def test_python_refuses_what_is_not_on_the_gpu():

@@ -232,6 +232,26 @@ def test_every_bit_of_fp32_inputs_counts_in_a_step(P, B, G, heads, dh, group):
     assert torch.equal(y, nxt)
 
 
+def test_products_with_the_codes_take_no_workspace(P):
+    """Many rows of bf16 allocate their outputs and nothing else, unless the weights are to be rounded."""
+    G, dh = 8, 2048
+    Wq = P.quantize_projection(weights(G, 1, dh, seed=51).cuda())
+    x = torch.randn(1, P.q4_exact_rows(dh, G, 1) + 1, dh, device="cuda").to(torch.bfloat16)
+
+    def extra():
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        u = P.input_projection_q4(x, Wq)
+        return torch.cuda.max_memory_allocated() - before - u.numel() * 2
+    try:
+        assert extra() < 1 << 20
+        P.set_q4_products(1)
+        assert extra() >= 2 * G * dh * dh
+    finally:
+        P.set_q4_products(0)
+
+
 def test_a_row_keeps_to_itself(P):
     """A NaN in one row, an infinity in another, both in one head: those rows of that head alone, in tiles as in single rows."""
     Wq = P.quantize_projection(weights(4, 3, 64, seed=9).cuda(), n_heads=3)
