@@ -497,7 +497,9 @@ int pararnn_gated_backward(int dtype, const void *u, const float *checkpoints, c
  *   scales bf16 [G][H][dh / group] chosen elsewhere.
  * pararnn_q4_dequantize: Wx fp32 [G][H][dh], code * scale (exact in fp32).
  * pararnn_input_projection_q4: u = B x + bias (bias fp32 [G][H] or NULL) for any number of rows.
- *   Products with the codes are exact, sums in fp32; fp32 storage: x in full (three bf16 terms).  workspace:
+ *   Products with the codes are exact, sums in fp32; fp32 storage: x in full (three bf16 terms).  bf16 storage: a code is multiplied as
+ *   24 + code and 24 times x taken out again, so that the fp32 sums, in h_next of a step too, round at up to eight times their
+ *   size: a few 1e-7 of sum |code scale x|.  B * L <= 1e9 (INVALID_ARG beyond).  u must not overlap x.  workspace:
  *   pararnn_q4_workspace_bytes() bytes (0 on invalid arguments), 256-byte aligned, or NULL where no weights are rounded:
  *   nothing else uses it.
  * pararnn_set_q4_products (host, process-wide; default 0): 0 as above; 1 allows bf16 storage of more than
@@ -507,7 +509,7 @@ int pararnn_gated_backward(int dtype, const void *u, const float *checkpoints, c
  * pararnn_gated_layer_step: one token of a gated layer in one launch: the projection followed by one step
  *   of the gated linear recurrence, h' = f h + i v with G = 2 or 3 as there.  x, y [B][H] in the storage
  *   type, h, h_next fp32 [B][H] (may be the same memory; h NULL = zeros), y = h' rounded.  u stays in fp32
- *   and is never written.  No workspace.
+ *   and is never written.  y must not overlap x.  B <= 1 048 576 (else UNSUPPORTED).  No workspace.
  * There are no gradients.  Device pointers; x 16-byte aligned (u too beyond pararnn_q4_exact_rows() rows of bf16), the others as
  * their elements.  A NaN or an infinity in x makes that row's outputs of that head NaN or infinite; so may finite inputs
  * or scales beyond 1e36 in magnitude, whose products overflow on the way.

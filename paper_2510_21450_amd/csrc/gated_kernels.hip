@@ -237,8 +237,9 @@ struct Place {
 
 // Chains are shared out among up to kQueues queues, neighbours to the same one: a queue hands out the tiles of its chains with a
 // ticket, along time first for none of them (all chains' first tiles, then all second ones).  One counter for all tiles
-// bounds a launch: its atomics take 12.5 ns each, 1.7 ms for 131072 tiles that move 6.4 GB.  Queue q's workgroups are
-// launched q, q + kQueues, ..., which are on one XCD, so that a line shared by two groups of channels is in its L2.
+// bounds a launch: its atomics take 12.5 ns each, 1.7 ms for 131072 tiles that move 6.4 GB.  Of 8 or 16 queues, queue q's workgroups
+// are launched q, q + queues, ..., which are on one XCD, so that a line shared by two groups of channels is in its L2; not the last
+// tiles of unequal queues (fewer than 16 chains' worth), nor those of another number of queues, which fewer than 16 chains make.
 // The last workgroup of a queue leaves the counter at zero for the next call.
 template <bool LOOK, bool REVERSE, int TT> __device__ __forceinline__ Place place_of(const GatedArgs &a, int *s_id)
 {

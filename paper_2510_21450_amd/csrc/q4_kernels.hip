@@ -7,7 +7,7 @@
 // A code becomes a bf16 number by one masked OR: the bits of q + 8 are put into the mantissa of 16, which gives
 // 24 + q, exactly.  The 24 is taken out by a product of the same x with -24, which the products of all gates start from:
 //   sum (24 + q) x - sum 24 x, each term exact in fp32, one more matrix instruction for each group of inputs.
-// Groups are scaled in fp32 as their sums are added up.  fp32 inputs are split into three bf16 terms (24 bits), and codes are
+// (What a sum carries is up to eight times larger for it, and its roundings with it.)  Groups are scaled in fp32 as their sums are added up.  fp32 inputs are split into three bf16 terms (24 bits), and codes are
 // operands without the 24, whose sums would lose three of those bits.
 #include <algorithm>
 #include <atomic>
@@ -257,8 +257,8 @@ template <> struct Eight<float> {
 // them and add up in LDS.  A row's inputs are read once for the NG CT tiles of weights and a weight once for the 16 MT rows.
 // Few rows are bound by the way to memory and back, so a wave asks for its units at once (its whole share of up to 4096 inputs for
 // one row), and for what it adds to the sums before the first of them comes.  G32: groups of 32 inputs, else of 64 and more.
-// One row, 3 x 4096 x 4096 weights (27 MB, not in a cache): 11 us, 2.4 TB/s; a step with 2 x 4096 x 4096 6.1, 2.9 TB/s;
-// launch, loads and sums of a small one 3.5 to 4.7 in a graph.
+// One row in a graph, weights read from memory: 3 x 4096 x 4096 (27 MB) 11 us, 2.4 TB/s; a step with 2 x 4096 x 4096 7.7, 2.3 TB/s; with the
+// weights in the memory-side cache 7.9 and 5.6.  Launch, loads and sums of a small one 3.0 to 4.3.
 template <typename T, int MT, int NG, int CT, bool STEP, bool G32>
 __global__ __launch_bounds__(512, MT * NG * CT == 1 ? 4 : 2) void q4_rows_kernel(const RowsQ4Args a)
 {
@@ -660,7 +660,7 @@ std::atomic<int> g_products{0};
 // take 8 us and, for every 256 tiles begun, 10 us and 1.4 for each 64 inputs of a head (2048 x 2 x 2048: 56 us for 65 rows, 61 for 2048,
 // 72 for 4096, 116 for 6000; 4096 x 3 x 1024: 41 to 45 up to 1024 rows, 73 for 2048, 106 for 4096); q4_tiles_kernel takes 2 us and 5 + 2.15 for
 // each 64 inputs, in proportion to the rows (46 us for 2048, 76 for 4096, 113 for 6000; 38, 64 and 120), with groups of 32 a fifth
-// more.  The projection takes over where it is ahead for a seventh of such a round at least, and never for heads of few inputs.
+// more.  The projection may take over where it is ahead for a seventh of such a round at least, and never for heads of few inputs.
 int exact_rows(int H, int G, int n_heads)
 {
     const double nu = H / n_heads / 64, round = 10.0 + 1.41 * nu, own = 5.0 + 2.15 * nu;
@@ -707,12 +707,6 @@ template <typename T, int MT, int NG, int CT, bool STEP> hipError_t launch_rows(
     else hipLaunchKernelGGL((q4_rows_kernel<T, MT, NG, CT, STEP, false>), grid, block, lds, st, a);
     return hipGetLastError();
 }
-constexpr int kWorkgroups = 192;        // fewer leave too much of the device idle
-// Rows and channels of a workgroup: the more, the fewer times weights and inputs are read, as long as there are workgroups for the
-// device.  bf16, 16 x 16 against 32 x 64 (a step: 32 x 16 of each gate): with 3 x 4096 x 4096 weights 11.1 us for one row and 16.1
-// for 16 against 11.8 and 12.0; a step with 2 x 8192 x 1024 5.7 and 6.9 against 5.6 and 5.7, with 2 x 4096 x 4096 7.3 and 9.3 against
-// 8.5 and 8.6; with too few workgroups, 3 x 2048 x 1024, 3.4 and 4.4 against 5.4 and 5.5.  fp32, whose terms cost more than the
-// weights: 4, 8 and 16 rows 17.3, 19.2 and 27.2 against 20.1, 19.4 and 19.4, a step with 2 x 4096 x 4096 10.5, 10.7 and 12.4 against 14.7.
 // Whether tiles of 128 rows beat the kernel of few rows.  They use a weight for twice the rows or more and need no sums of eight waves, but have
 // fewer workgroups, which take a unit in 0.7 us (fp32 2.9): it pays from a number of the latter's workgroups (64 rows x 64 channels,
 // fp32 32 x 64) on.  Both level, bf16, units of a head: that number: 1: 90, 4: 340, 8: 300, 11: 340, 16: 390, 32: 580; 4096 rows: 9.9 to
@@ -751,6 +745,13 @@ template <typename T> hipError_t launch_tiles(const RowsQ4Args &a, int group, hi
         return launch_tiles<T, 4, 2, 1>(a, narrow, group, st);
     }
 }
+constexpr int kWorkgroups = 192;        // fewer leave too much of the device idle
+// Rows and channels of a workgroup: the more, the fewer times weights and inputs are read, as long as there are workgroups for the
+// device.  In a graph, weights read from memory, one row and 16 of bf16, 16 x 16 against 32 x 64 (a step: 32 x 16 of each gate): 3 x 4096 x 4096
+// 11.4 us and 15.9 against 10.8 and 10.9 (weights in the memory-side cache 8.4 and 15.0 against 9.6 and 9.7), a step with 2 x 8192 x 1024 6.3 and 7.4
+// against 6.3 and 6.5, with 2 x 4096 x 4096 7.9 and 9.2 against 8.7 and 8.9; with too few workgroups, 3 x 2048 x 1024, 3.9 and 5.1
+// against 5.5 twice.  fp32, whose terms cost more than the weights, 4, 8 and 16 rows: 18.2, 19.5 and 27.5 against 20.0, 19.9 and
+// 20.1, a step with 2 x 4096 x 4096 11.0, 10.9 and 12.8 against 15.0.
 template <typename T, int NG, bool STEP> hipError_t launch_rows_of(RowsQ4Args a, int n_heads, int group, hipStream_t st)
 {
     a.dh = a.H / n_heads; a.nu = a.dh / 64; a.ng = a.dh / group; a.tiles = (unsigned)a.H / 16;
@@ -759,9 +760,9 @@ template <typename T, int NG, bool STEP> hipError_t launch_rows_of(RowsQ4Args a,
     auto enough = [&](int mt, int ct) { return tiles / ct * ((a.rows + 16 * mt - 1) / (16 * mt)) >= kWorkgroups; };
     constexpr int C4 = STEP ? 1 : 4;
     constexpr bool bf16 = sizeof(T) == 2;
-    // (three terms of fp32 leave no registers for 64 rows: 46 -> 88 us for 64 of 3 x 4096 x 4096)
     if constexpr (!STEP)
         if (tiles_better(a, bf16)) return launch_tiles<T>(a, group, st);
+    // (three terms of fp32 leave no registers for 64 rows: 46 -> 88 us for 64 of 3 x 4096 x 4096)
     if constexpr (bf16)
         if (a.rows > 32 && enough(4, C4)) return launch_rows<T, 4, NG, C4, STEP>(a, group, st);
     if (a.rows > (bf16 || !STEP ? 8 : 16) && enough(2, C4)) return launch_rows<T, 2, NG, C4, STEP>(a, group, st);
